@@ -422,6 +422,118 @@ int sirius_generate(const sirius_model* model, int32_t* seq, int32_t* cache_pos,
                     int periods, int32_t* out_tokens, int32_t* out_count,
                     const sirius_gen_trace* trace, void* ws, size_t ws_bytes, void* stream);
 
+/* Element types of the entry points below that take more than one. */
+#define SIRIUS_F32 0
+#define SIRIUS_BF16 1
+
+/*
+ * Rotary positions: which columns of a head turn, by what, and the norm before.
+ *   freqs       DEVICE [rot_dim / 2] doubles, radians per position (sirius_rope_freqs
+ *               computes the usual ones on the host); may be NULL when rot_dim = 0.
+ *   rot_dim     the first rot_dim columns turn (even, 0 .. head_dim), the rest pass.
+ *   interleaved 0: pair j is columns (j, j + rot_dim / 2); else (2 j, 2 j + 1).
+ *   mscale      factor on the turned columns (1; some long-context scalings use
+ *               0.1 ln(factor) + 1).
+ *   norm_eps    >= 0: RMSNorm of every head first, x / sqrt(mean(x^2) + eps) * w; < 0: none.
+ *   q_weight, k_weight [head_dim] bf16, the norm's weights, or NULL for ones.
+ */
+typedef struct sirius_rotation {
+  const double* freqs;
+  const uint16_t* q_weight;
+  const uint16_t* k_weight;
+  int rot_dim, interleaved;
+  float mscale, norm_eps;
+} sirius_rotation;
+
+#define SIRIUS_ROPE_PLAIN 0
+#define SIRIUS_ROPE_LINEAR 1
+#define SIRIUS_ROPE_BASE 2
+#define SIRIUS_ROPE_SMOOTH 3
+#define SIRIUS_ROPE_RAMP 4
+/*
+ * Frequencies on the HOST: freqs[j] = theta^(-2 j / rot_dim), j < rot_dim / 2, scaled for
+ * contexts `factor` times as long by one of
+ *   LINEAR  f / factor;
+ *   BASE    theta replaced by theta factor^(rot_dim / (rot_dim - 2)) (rot_dim > 2);
+ *   SMOOTH  with w = orig_len f / (2 pi) turns over the original length and
+ *           s = (w - low) / (high - low) clamped to [0, 1]: f (s + (1 - s) / factor);
+ *   RAMP    the same between pair indices instead of turns: s falls linearly from 1 at
+ *           index floor(d(high)) to 0 at ceil(d(low)), d(w) = rot_dim ln(orig_len / (2 pi w)) /
+ *           (2 ln theta), both clamped to [0, rot_dim - 1].
+ * factor, low, high, orig_len are ignored where the scaling does not name them.
+ * Errors: SIRIUS_EINVAL for a null pointer, rot_dim odd or outside [2, 128], theta not finite
+ * or <= 1, an unknown scaling, factor not finite or < 1, low < 0, high <= low, orig_len < 1.
+ */
+int sirius_rope_freqs(double* freqs, int rot_dim, double theta, int scaling, double factor,
+                      double low, double high, double orig_len);
+
+/*
+ * Positions into queries and keys (what sirius_attn_kv expects to have been done): each head's
+ * row is normalised (optional) and its pairs turn by positions[t] * freqs[j]:
+ *   (u, v) -> mscale (u cos a - v sin a, u sin a + v cos a)
+ * Angles are formed and reduced in fp64, everything else is fp32 with one rounding at the end.
+ *   q     [T, H, head_dim] of q_dtype, tokens ldq elements apart (>= H head_dim, a multiple
+ *         of 8: a view into a wider projection works); NULL: keys only.
+ *   k     [T, Hkv, head_dim] of k_dtype, tokens ldk apart; NULL: queries only.
+ *   positions [T] int32 on the device.
+ *   q_out [T, H, head_dim] of q_dtype, contiguous; may be q itself when ldq = H head_dim.
+ *   k_out [T, Hkv, head_dim] bf16, contiguous (the type of every key cache here); may be k when
+ *         k is bf16 and ldk = Hkv head_dim.
+ * T == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null or misaligned (16 bytes) pointers, an
+ * unknown dtype, head_dim not a multiple of 8 in [8, 128], H or Hkv outside [1, 4096], T outside
+ * [0, 2^20], a bad stride, and a bad rotation (rot_dim odd or outside [0, head_dim], mscale not
+ * finite, norm_eps NaN).
+ */
+int sirius_rope(const void* q, int q_dtype, int64_t ldq, const void* k, int k_dtype, int64_t ldk,
+                const int32_t* positions, int T, int H, int Hkv, int head_dim,
+                const sirius_rotation* rotation, void* q_out, uint16_t* k_out, void* stream);
+
+/*
+ * A key/value cache in pages, and where a call's T tokens go in it. Sequence b has the pages
+ * page_table[b, 0 ..] of the pool: its row r lies in page page_table[b, r / page_size] at offset
+ * r % page_size. Its tokens in this call are tok_start[b] .. tok_start[b + 1] - 1 and stand at rows
+ * cache_pos[b], cache_pos[b] + 1, ... (sirius_kv_rollback moves cache_pos afterwards). Values are
+ * stored transposed, a column's positions side by side, as the matrix products read them.
+ *   k_pages [n_pages, n_kv_heads, page_size, head_dim] bf16
+ *   v_pages [n_pages, n_kv_heads, head_dim, page_size] bf16
+ *   page_table [B, max_pages] int32; pages may be shared by sequences that only read them
+ *   cache_pos  [B] int32
+ *   tok_start  [B + 1] int32, ascending from 0, or NULL: max_n tokens each, T = B max_n.
+ *   max_n      at least the longest sequence's tokens in this call.
+ * All pointers are device pointers. Tokens at or behind tok_start[B] belong to no sequence: their
+ * outputs are left as they were. Limits: page_size a multiple of 8 in [8, 4096], max_pages *
+ * page_size <= 2^20, head_dim a multiple of 8 in [8, 128], B <= 65535, T <= 2^20.
+ */
+typedef struct sirius_paged {
+  uint16_t* k_pages;
+  uint16_t* v_pages;
+  const int32_t* page_table;
+  const int32_t* cache_pos;
+  const int32_t* tok_start;
+  int B, T, max_n;
+  int n_kv_heads, head_dim;
+  int n_pages, page_size, max_pages;
+} sirius_paged;
+
+/*
+ * The append: queries are rotated out, keys are rotated on the way into their cache rows, values
+ * are written beside them (rounded to bf16 from fp32 inputs). A token's position is its cache row,
+ * or positions[t] (drafted trees: nodes of one level share a position).
+ *   q, q_out as in sirius_rope (q may be NULL: keys and values only).
+ *   k, v     [T, n_kv_heads, head_dim] of kv_dtype, tokens ldk, ldv elements apart.
+ *   positions [T] int32 on the device, or NULL.
+ *   rotation  may be NULL: no norm, nothing turns.
+ * A sequence with cache_pos < 0 or tokens behind its table's last row writes nothing, nor does a
+ * token whose page is outside [0, n_pages); queries are written all the same. Two tokens must
+ * not fall on one row of one page. T == 0 and B == 0 are valid no-ops.
+ * Errors: as sirius_rope, plus SIRIUS_EINVAL for the cache's limits above, and T != B max_n without
+ * tok_start.
+ */
+int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, const void* v,
+                     int kv_dtype, int64_t ldk, int64_t ldv, const sirius_paged* cache,
+                     const int32_t* positions, int H, const sirius_rotation* rotation,
+                     void* q_out, void* stream);
+
 /*
  * RMSNorm with unit weight, the layer-stack glue around the FFN:
  *   out[b] = h[b] / sqrt(mean(h[b]^2) + eps). out may alias h.
@@ -460,7 +572,7 @@ int sirius_fill_normal_bf16(uint16_t* out, size_t n, uint64_t seed, float mean, 
  * "topk_gate", "topk_cut"; "verify_stats", "verify_scan", "tree_stats", "tree_scan",
  * "tree_topw", "tree_select"; "griffin_z", "griffin_rownorm", "griffin_score",
  * "griffin_topk", "condense"; "rmsnorm", "fill_normal"; "attn_partial",
- * "attn_combine", "kv_rollback".
+ * "attn_combine", "kv_rollback"; "rope", "kv_append".
  * sirius_profile_reset drops every record (it waits for pending events).
  * Errors: SIRIUS_EINVAL for NULL arguments, SIRIUS_EHIP if an event fails.
  */

@@ -19,6 +19,8 @@ A plain, slow, float64 NumPy statement of what the GPU library computes:
                 decoder: drafting by the sparse model, the full model's
                 check with the direct cache rewrite, rollback and
                 interleaving of the corrected token;
+  * serve    -- the batched serving step: rotary positions, the append to a
+                paged cache, attention over it, sampling;
   * apu      -- the efficiency bookkeeping of Sec. 2.2 and Sec. 2.3
                 (APU, effective density, speculative-decoding AAL).
 
@@ -57,3 +59,4 @@ from .tree import log_softmax, tree_build_step, tree_paths, tree_verify  # noqa:
 from .apu import sd_aal, apu, effective_density  # noqa: F401
 from .kv import attn_kv, kv_rollback  # noqa: F401
 from . import loop  # noqa: F401
+from . import serve  # noqa: F401

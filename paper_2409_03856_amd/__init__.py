@@ -22,6 +22,9 @@ from ._lib import (  # noqa: F401
     sirius_tree_verify,
     sirius_attn_kv,
     sirius_kv_rollback,
+    sirius_rope_freqs,
+    sirius_rope,
+    sirius_kv_append,
     sirius_rmsnorm,
     Model,
     sirius_model_workspace_size,

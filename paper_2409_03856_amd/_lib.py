@@ -21,6 +21,9 @@ SIRIUS_EINVAL = -1
 SIRIUS_EWORKSPACE = -2
 SIRIUS_EHIP = -3
 
+SIRIUS_F32 = 0
+SIRIUS_BF16 = 1
+
 OP_FFN_DENSE = 0
 OP_FFN_CATS = 1
 OP_GRIFFIN_SELECT = 2
@@ -36,6 +39,8 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
 _Z = ctypes.c_size_t
+_D = ctypes.c_double
+_L = ctypes.c_int64
 
 # name -> (restype, argtypes), in the order of include/sirius.h
 SIGNATURES = {
@@ -54,6 +59,9 @@ SIGNATURES = {
     "sirius_model_workspace_size": (_Z, [_P, _I]),
     "sirius_model_forward": (_I, [_P, _P, _I, _P, _I, _P, _P, _P, _P, _Z, _P]),
     "sirius_generate": (_I, [_P, _P, _P, _I, _F, _I, _P, _P, _P, _P, _Z, _P]),
+    "sirius_rope_freqs": (_I, [_P, _I, _D, _I, _D, _D, _D, _D]),
+    "sirius_rope": (_I, [_P, _I, _L, _P, _I, _L, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
+    "sirius_kv_append": (_I, [_P, _I, _L, _P, _P, _I, _L, _L, _P, _P, _I, _P, _P, _P]),
     "sirius_rmsnorm": (_I, [_P, _I, _I, _F, _P, _P]),
     "sirius_fill_normal_bf16": (_I, [_P, _Z, ctypes.c_uint64, _F, _F, _P]),
     "sirius_profile_enable": (_I, [_I]),
@@ -498,6 +506,193 @@ def sirius_kv_rollback(cache_pos, accept_len, n, *, stream=None):
     _check(lib().sirius_kv_rollback(_ptr(cache_pos), _ptr(accept_len), int(cache_pos.shape[0]), int(n),
                                     _handle()))
     return cache_pos
+
+
+# ---------------------------------------------------------------- the batched serving step
+
+class _RotationC(ctypes.Structure):
+    """struct sirius_rotation of include/sirius.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("freqs", "q_weight", "k_weight")] + \
+               [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("mscale", _F), ("norm_eps", _F)]
+
+
+class _PagedC(ctypes.Structure):
+    """struct sirius_paged of include/sirius.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "cache_pos", "tok_start")] + \
+               [(n, ctypes.c_int) for n in ("B", "T", "max_n", "n_kv_heads", "head_dim", "n_pages", "page_size",
+                                            "max_pages")]
+
+
+def _elsewhere(t):
+    """Whether t lives on another GPU than torch's current one."""
+    return t.is_cuda and t.device.index != _torch().cuda.current_device()
+
+
+def _there(t, entry, args: dict):
+    """entry(**args) with t's GPU as the current one."""
+    with _torch().cuda.device(t.device):
+        return entry(**args)
+
+
+def _dtype(t) -> int:
+    torch = _torch()
+    if t.dtype is torch.float32:
+        return SIRIUS_F32
+    _need(t.dtype is torch.bfloat16, "tensors must be fp32 or bf16")
+    return SIRIUS_BF16
+
+
+def _rows(t, name):
+    """(tokens, heads, head size, elements between tokens) of [T, heads, hd] whose tokens may be apart."""
+    _need(t.dim() == 3, f"{name} must be [T, heads, head_dim]")
+    n, h, d = t.shape
+    s = t.stride()
+    _need(t.is_cuda, "tensors must live on the GPU")
+    _need(n == 0 or (s[2] == 1 and (h == 1 or s[1] == d)), f"the heads of a token of {name} must be contiguous")
+    return n, h, d, s[0] if n > 1 else h * d
+
+
+def _same_device(first, *ts):
+    for t in ts:
+        _need(t is None or t.device == first.device, "tensors must live on one GPU")
+
+
+def _int32(t, shape, name):
+    _need(t.dtype is _torch().int32 and tuple(t.shape) == shape and t.is_contiguous(),
+          f"{name} must be int32 {list(shape)}, contiguous")
+
+
+def _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd):
+    torch = _torch()
+    half = 0
+    if freqs is not None:
+        _need(freqs.dtype is torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and 2 * freqs.numel() <= hd,
+              "freqs must be float64 [rot_dim / 2], rot_dim at most head_dim")
+        half = freqs.numel()
+    for w in (q_weight, k_weight):
+        if w is not None:
+            _need(w.dtype is torch.bfloat16 and tuple(w.shape) == (hd,) and w.is_contiguous(),
+                  "norm weights must be bf16 [head_dim]")
+    return _RotationC(_ptr(freqs) if half else None, _ptr(q_weight), _ptr(k_weight), 2 * half, 1 if interleaved else 0,
+                      mscale, norm_eps)
+
+
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "smooth": 3, "ramp": 4}
+
+
+def sirius_rope_freqs(rot_dim, theta=10000.0, *, scaling="none", factor=1.0, low=1.0, high=4.0, orig_len=8192,
+                      device=None):
+    """The rotation's frequencies, float64 [rot_dim / 2] on the device (torch's current GPU by default).
+    scaling: "none", "linear", "base", "smooth" or "ramp" (SIRIUS_ROPE_* of include/sirius.h)."""
+    torch = _torch()
+    _need(scaling in _ROPE_SCALINGS, f"scaling must be one of {', '.join(_ROPE_SCALINGS)}")
+    _need(int(rot_dim) > 0, "rot_dim must be positive")
+    host = torch.empty(int(rot_dim) // 2, dtype=torch.float64)
+    _check(lib().sirius_rope_freqs(host.data_ptr() or None, int(rot_dim), float(theta), _ROPE_SCALINGS[scaling], float(factor),
+                                   float(low), float(high), float(orig_len)))
+    return host.to("cuda" if device is None else device)
+
+
+def sirius_rope(q, k, positions, freqs, *, interleaved=False, mscale=1.0, norm_eps=-1.0, q_weight=None, k_weight=None,
+                q_out=None, k_out=None, stream=None):
+    """q [T, H, hd] and k [T, Hkv, hd] (fp32 or bf16, tokens may be apart, either may be None),
+    positions [T] int32, freqs float64 [rot_dim / 2] (sirius_rope_freqs). Returns (q_out of q's type,
+    k_out bf16), contiguous, or None in the place of an absent input."""
+    if stream is not None:
+        return _on(stream, sirius_rope, locals())
+    _need(q is not None or k is not None, "q and k are both None")
+    first = q if q is not None else k
+    if _elsewhere(first):
+        args = dict(locals())
+        del args["first"]
+        return _there(first, sirius_rope, args)
+    torch = _torch()
+    t, h, hkv, hd, ldq, ldk = int(first.shape[0]), 1, 1, int(first.shape[-1]), 0, 0
+    qt = kt = SIRIUS_F32
+    if q is not None:
+        t, h, hd, ldq = _rows(q, "q")
+        qt = _dtype(q)
+        if q_out is None:
+            q_out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
+        _need(q_out.dtype is q.dtype and q_out.shape == q.shape and q_out.is_contiguous(),
+              "q_out must be like q, contiguous")
+    else:
+        q_out = None
+    if k is not None:
+        tk, hkv, dk, ldk = _rows(k, "k")
+        _need(q is None or (tk == t and dk == hd), "q and k disagree on T or head_dim")
+        kt = _dtype(k)
+        if k_out is None:
+            k_out = torch.empty((tk, hkv, dk), dtype=torch.bfloat16, device=k.device)
+        _need(k_out.dtype is torch.bfloat16 and k_out.shape == k.shape and k_out.is_contiguous(),
+              "k_out must be bf16 [T, Hkv, head_dim], contiguous")
+    else:
+        k_out = None
+    _int32(positions, (t,), "positions")
+    _same_device(first, k, positions, freqs, q_weight, k_weight, q_out, k_out)
+    rot = _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
+    _check(lib().sirius_rope(_ptr(q), qt, ldq, _ptr(k), kt, ldk, _ptr(positions), t, h, hkv, hd, ctypes.byref(rot),
+                             _ptr(q_out), _ptr(k_out), _handle()))
+    return q_out, k_out
+
+
+def _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n):
+    """The call's sirius_paged: T tokens of head size hd, max_n of a sequence at most (None: T, or T / B)."""
+    torch = _torch()
+    _need(k_pages.dtype is torch.bfloat16 and v_pages.dtype is torch.bfloat16 and k_pages.dim() == 4 and v_pages.dim() == 4
+          and k_pages.is_contiguous() and v_pages.is_contiguous(), "k_pages and v_pages must be contiguous bf16 [pages, ...]")
+    pages, hkv, size, d = k_pages.shape
+    _need(d == hd and v_pages.shape == (pages, hkv, d, size),
+          "pages must be [pages, Hkv, page_size, head_dim] (keys) and [pages, Hkv, head_dim, page_size] (values)")
+    _need(page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
+          "page_table must be int32 [B, pages per sequence], contiguous")
+    bsz, wide = page_table.shape
+    _int32(cache_pos, (bsz,), "cache_pos")
+    if tok_start is not None:
+        _int32(tok_start, (bsz + 1,), "tok_start")
+        n = t if max_n is None else int(max_n)
+    else:
+        _need(bsz == 0 or t % bsz == 0, "without tok_start every sequence has T / B tokens")
+        n = t // bsz if bsz else 0
+        _need(max_n is None or max_n >= n, "max_n is less than T / B")
+    return _PagedC(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_pos), _ptr(tok_start), bsz, t, n, hkv, d,
+                   pages, size, wide)
+
+
+def sirius_kv_append(q, k, v, k_pages, v_pages, page_table, cache_pos, freqs=None, *, tok_start=None, positions=None,
+                     interleaved=False, mscale=1.0, norm_eps=-1.0, q_weight=None, k_weight=None, q_out=None, stream=None):
+    """Rotates q [T, H, hd] (None: keys and values only) and k [T, Hkv, hd], and writes k and v to the
+    sequences' cache rows cache_pos[b] .. in k_pages [pages, Hkv, page_size, hd] and v_pages [pages, Hkv, hd,
+    page_size] (bf16, updated in place). page_table [B, pages per sequence], cache_pos [B], tok_start
+    [B + 1] or None (T / B tokens each), positions [T] or None (the cache rows): int32. Returns q_out."""
+    if stream is not None:
+        return _on(stream, sirius_kv_append, locals())
+    if _elsewhere(k):
+        return _there(k, sirius_kv_append, locals())
+    torch = _torch()
+    t, hkv, hd, ldk = _rows(k, "k")
+    tv, hv, dv, ldv = _rows(v, "v")
+    _need(tv == t and hv == hkv and dv == hd and v.dtype is k.dtype, "k and v must be alike")
+    _need(hkv == k_pages.shape[1], "k and the pages disagree on the number of heads")
+    h, ldq, qt = 1, 0, SIRIUS_F32
+    if q is not None:
+        tq, h, dq, ldq = _rows(q, "q")
+        _need(tq == t and dq == hd, "q and k disagree on T or head_dim")
+        qt = _dtype(q)
+        if q_out is None:
+            q_out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
+        _need(q_out.dtype is q.dtype and q_out.shape == q.shape and q_out.is_contiguous(),
+              "q_out must be like q, contiguous")
+    else:
+        q_out = None
+    if positions is not None:
+        _int32(positions, (t,), "positions")
+    _same_device(k, q, v, k_pages, v_pages, page_table, cache_pos, tok_start, positions, freqs, q_weight, k_weight, q_out)
+    cache = _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, None)
+    rot = _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
+    _check(lib().sirius_kv_append(_ptr(q), qt, ldq, _ptr(k), _ptr(v), _dtype(k), ldk, ldv, ctypes.byref(cache),
+                                  _ptr(positions), h, ctypes.byref(rot), _ptr(q_out), _handle()))
+    return q_out
 
 
 def sirius_rmsnorm(h, eps=1e-5, *, out=None, stream=None):

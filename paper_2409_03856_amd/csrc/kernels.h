@@ -224,6 +224,30 @@ hipError_t launch_attn_kv(const float* q, const uint16_t* k_new, const uint16_t*
 hipError_t launch_kv_rollback(int32_t* cache_pos, const int32_t* accept_len, int B, int n,
                               hipStream_t stream);
 
+// ---- the paged cache: rotation, append, attention; sampling
+struct PagedView;  // paged.h
+// Rows of heads to rotate: q [T][H][hd] (token stride ldq) to q_out [T][H][hd] of the same type; k to k_out
+// [T][Hkv][hd] bf16, or with a cache k and v to its pages. q may be null, k without a cache too. hd % 8 == 0,
+// strides % 8 == 0, every pointer 16-byte aligned; eps < 0: no norm; positions may be null with a cache.
+struct RopeCall {
+  const void* q;
+  const void* k;
+  const void* v;
+  bool q_bf16, k_bf16;
+  long ldq, ldk, ldv;
+  const int32_t* positions;
+  int T, H, Hkv, hd;
+  const double* freqs;
+  int rot, inter;
+  float mscale, eps;
+  const uint16_t* qw;
+  const uint16_t* kw;
+  void* q_out;
+  uint16_t* k_out;
+};
+hipError_t launch_rope(const RopeCall& c, hipStream_t stream);
+hipError_t launch_kv_append(const RopeCall& c, const PagedView& pg, hipStream_t stream);
+
 // ---- small decoder and the generation loop (model.hip)
 // h[i] = E[tokens[i]] widened to fp32 (0 for an id outside [0, V)); d % 8 == 0.
 hipError_t launch_embed(const int32_t* tokens, int n, const uint16_t* E, int d, int V, float* out,

@@ -1,0 +1,103 @@
+"""Refusals of the serving-step entry points, on the host before anything is enqueued."""
+
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(
+    not os.path.exists(os.path.join(ROOT, "paper_2409_03856_amd", "libsirius.so")),
+    reason="libsirius.so not built (run __graft_entry__.build())")
+
+FAKE = ctypes.c_void_p(1 << 20)  # non-null, 16-byte aligned; never dereferenced by these calls
+ODD = ctypes.c_void_p((1 << 20) + 8)
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2409_03856_amd import _lib
+    return _lib
+
+
+def _rotation(lib, **kw):
+    r = dict(freqs=1 << 20, q_weight=None, k_weight=None, rot_dim=64, interleaved=0, mscale=1.0, norm_eps=-1.0)
+    return lib._RotationC(*(r | kw).values())
+
+
+def _paged(lib, **kw):
+    c = dict(k_pages=1 << 20, v_pages=1 << 21, page_table=1 << 20, cache_pos=1 << 20, tok_start=None, B=2, T=6, max_n=3,
+             n_kv_heads=2, head_dim=64, n_pages=9, page_size=16, max_pages=4)
+    return lib._PagedC(*(c | kw).values())
+
+
+BAD_ROTATIONS = [dict(rot_dim=7), dict(rot_dim=66), dict(rot_dim=-2), dict(freqs=None), dict(mscale=NAN), dict(mscale=INF),
+                 dict(norm_eps=NAN), dict(norm_eps=INF), dict(q_weight=(1 << 20) + 2), dict(freqs=(1 << 20) + 8)]
+BAD_CACHES = [dict(k_pages=None), dict(v_pages=None), dict(k_pages=(1 << 20) + 8), dict(page_table=None), dict(cache_pos=None),
+              dict(B=-1), dict(B=65536, T=65536 * 3), dict(T=-1), dict(T=5), dict(T=(1 << 20) + 1, max_n=1 << 20, B=1),
+              dict(max_n=-1), dict(n_kv_heads=0), dict(head_dim=12), dict(head_dim=136), dict(n_pages=0), dict(page_size=12),
+              dict(page_size=0), dict(page_size=4104), dict(max_pages=0), dict(max_pages=65537)]
+
+
+def test_rope_refusals(lib):
+    L = lib.lib()
+    base = dict(q=FAKE, qt=0, ldq=256, k=FAKE, kt=1, ldk=128, pos=FAKE, T=3, H=4, Hkv=2, hd=64, rot=_rotation(lib), qo=FAKE, ko=FAKE)
+
+    def call(**kw):
+        a = base | kw
+        a["rot"] = None if a["rot"] is None else ctypes.byref(a["rot"])
+        return L.sirius_rope(*a.values(), None)
+
+    for kw in (dict(q=None, k=None), dict(q=ODD), dict(qo=None), dict(qo=ODD), dict(k=ODD), dict(ko=None), dict(pos=None), dict(qt=2),
+               dict(kt=-1), dict(ldq=255), dict(ldq=252), dict(ldq=260), dict(ldk=64), dict(T=-1), dict(T=(1 << 20) + 1), dict(H=0),
+               dict(H=4097), dict(Hkv=0), dict(hd=60), dict(hd=0), dict(hd=136), dict(rot=None)):
+        assert call(**kw) == -1, kw
+    for kw in BAD_ROTATIONS:
+        assert call(rot=_rotation(lib, **kw)) == -1, kw
+    assert call(T=0, q=None, k=None) == 0
+
+
+def test_append_refusals(lib):
+    L = lib.lib()
+    base = dict(q=FAKE, qt=0, ldq=256, k=FAKE, v=FAKE, kt=1, ldk=128, ldv=128, cache=_paged(lib), pos=None, H=4,
+                rot=_rotation(lib), qo=FAKE)
+
+    def call(**kw):
+        a = base | kw
+        for n in ("rot", "cache"):
+            a[n] = None if a[n] is None else ctypes.byref(a[n])
+        return L.sirius_kv_append(*a.values(), None)
+
+    for kw in (dict(k=None), dict(v=None), dict(k=ODD), dict(v=ODD), dict(q=ODD), dict(qo=None), dict(qt=3), dict(kt=2), dict(ldk=120),
+               dict(ldv=132), dict(ldq=128), dict(H=0), dict(cache=None)):
+        assert call(**kw) == -1, kw
+    for kw in BAD_CACHES:
+        assert call(cache=_paged(lib, **kw)) == -1, kw
+    for kw in BAD_ROTATIONS:
+        assert call(rot=_rotation(lib, **kw)) == -1, kw
+    for kw in (dict(T=0, B=0), dict(T=0, max_n=0), dict(T=0, tok_start=1 << 20)):
+        assert call(cache=_paged(lib, **kw), k=None) == 0, kw
+
+
+def test_binding_refusals(lib):
+    """Shapes and types that the binding turns away before the library sees them (tensors on the CPU are among them)."""
+    import torch
+    x = torch.zeros(3, 4, 64)
+    pos = torch.zeros(3, dtype=torch.int32)
+    f = torch.ones(32, dtype=torch.float64)
+    with pytest.raises(ValueError, match="GPU"):
+        lib.sirius_rope(x, x, pos, f)
+    with pytest.raises(ValueError):
+        lib.sirius_rope(None, None, pos, f)
+    with pytest.raises(ValueError, match="heads, head_dim"):
+        lib.sirius_rope(x[0], None, pos, f)
+    pages, table = torch.zeros(2, 4, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        lib.sirius_kv_append(None, x, x, pages, pages.transpose(2, 3), table, pos[:1], f)
+    with pytest.raises(ValueError):
+        lib.sirius_rope_freqs(64, scaling="half")
+    with pytest.raises(ValueError):
+        lib.sirius_rope_freqs(0)
+    with pytest.raises(lib.SiriusError):
+        lib.sirius_rope_freqs(64, 0.5)
