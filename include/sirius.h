@@ -61,6 +61,7 @@ extern "C" {
 #define SIRIUS_OP_TREE_VERIFY 7
 #define SIRIUS_OP_FFN_TOPK 8
 #define SIRIUS_OP_ATTN_KV 9
+#define SIRIUS_OP_ATTN_PAGED 10
 
 /*
  * Dense SwiGLU FFN (the full model, sparsity 0):
@@ -535,6 +536,38 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
                      void* q_out, void* stream);
 
 /*
+ * Attention over the paged cache, after the append: token i of sequence b (cache row p + i, p =
+ * cache_pos[b]) attends to rows 0 .. p + i,
+ *   out[t,h] = sum_j softmax_j(s_j) V[j, h / G],  s_j = scale q[t,h] . K[j, h / G],  G = H / n_kv_heads,
+ * one token per sequence (decoding), a drafted chunk, a drafted tree or a prompt. Any of:
+ *   softcap > 0   s <- softcap tanh(s / softcap);
+ *   slopes        s <- s - slopes[h] (p + i - j), after the cap: a bias by distance in rows;
+ *   window > 0    only rows j > p + i - window are seen;
+ *   mask          [T] words: of the chunk's own rows p + c token t sees those with bit c set (its
+ *                 own too; rows below p by the rules above). The bits of a node's ancestors make
+ *                 this the pass over a drafted tree that sirius_tree_verify checks. max_n <= 64.
+ *   q      [T, H, head_dim] of q_dtype, tokens ldq elements apart.
+ *   scale  > 0, or 0 for 1 / sqrt(head_dim).
+ *   slopes [H] fp32 on the device, or NULL.
+ *   out    [T, H, head_dim] of q_dtype, contiguous.
+ * A token that sees no row, or only rows of score -infinity, gets zeros. What is hidden from a token
+ * does not reach it, whatever it holds, nor do rows behind a sequence's last token. A sequence with
+ * cache_pos < 0, tokens behind its table's last row, or more than max_n tokens gets NaN, and so do
+ * the tokens that see a row on a page outside [0, n_pages) (the sequence's other tokens may);
+ * pages in front of every token's window are not looked at.
+ * Scores, softmax and the weighted sum are fp32 on the stored bf16 keys and values: fp32 queries and
+ * probabilities enter the matrix products in pieces that hold every bit, and with bf16 queries the
+ * probabilities hold 16 bits.
+ * Needs sirius_workspace_size(SIRIUS_OP_ATTN_PAGED, ...) for the call's B and max_n.
+ * T == 0 and B == 0 are valid no-ops. Errors: SIRIUS_EINVAL as sirius_kv_append for q and the
+ * cache, H not a multiple of n_kv_heads, scale < 0 or not finite, softcap < 0 or not finite,
+ * window < 0, a mask with max_n > 64, too many query rows per call; SIRIUS_EWORKSPACE.
+ */
+int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_paged* cache, int H,
+                      float scale, float softcap, const float* slopes, int window,
+                      const uint64_t* mask, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * RMSNorm with unit weight, the layer-stack glue around the FFN:
  *   out[b] = h[b] / sqrt(mean(h[b]^2) + eps). out may alias h.
  * Errors: SIRIUS_EINVAL for null pointers, d_model < 1, eps < 0.
@@ -572,7 +605,8 @@ int sirius_fill_normal_bf16(uint16_t* out, size_t n, uint64_t seed, float mean, 
  * "topk_gate", "topk_cut"; "verify_stats", "verify_scan", "tree_stats", "tree_scan",
  * "tree_topw", "tree_select"; "griffin_z", "griffin_rownorm", "griffin_score",
  * "griffin_topk", "condense"; "rmsnorm", "fill_normal"; "attn_partial",
- * "attn_combine", "kv_rollback"; "rope", "kv_append".
+ * "attn_combine", "kv_rollback"; "rope", "kv_append",
+ * "attn_paged", "attn_paged_merge".
  * sirius_profile_reset drops every record (it waits for pending events).
  * Errors: SIRIUS_EINVAL for NULL arguments, SIRIUS_EHIP if an event fails.
  */
@@ -589,6 +623,7 @@ int sirius_profile_query(const char* kernel, double* total_ms, int64_t* launches
  *   TREE_BUILD: B, Wc, W, V, unused
  *   TREE_VERIFY: B, K, W, V, bonus
  *   ATTN_KV: B, n, H * 65536 + Hkv, head_dim, Lmax
+ *   ATTN_PAGED: B, max_n, H * 65536 + n_kv_heads, head_dim, unused
  * Returns 0 for an unknown op or invalid sizes. */
 size_t sirius_workspace_size(int op, int B, int d_model, int d_ff, int T_or_V, int K_or_R);
 

@@ -25,6 +25,7 @@ from ._lib import (  # noqa: F401
     sirius_rope_freqs,
     sirius_rope,
     sirius_kv_append,
+    sirius_attn_paged,
     sirius_rmsnorm,
     Model,
     sirius_model_workspace_size,
@@ -47,4 +48,5 @@ from ._lib import (  # noqa: F401
     OP_TREE_VERIFY,
     OP_FFN_TOPK,
     OP_ATTN_KV,
+    OP_ATTN_PAGED,
 )

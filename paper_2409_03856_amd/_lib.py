@@ -34,6 +34,7 @@ OP_TREE_BUILD = 6
 OP_TREE_VERIFY = 7
 OP_FFN_TOPK = 8
 OP_ATTN_KV = 9
+OP_ATTN_PAGED = 10
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -62,6 +63,7 @@ SIGNATURES = {
     "sirius_rope_freqs": (_I, [_P, _I, _D, _I, _D, _D, _D, _D]),
     "sirius_rope": (_I, [_P, _I, _L, _P, _I, _L, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
     "sirius_kv_append": (_I, [_P, _I, _L, _P, _P, _I, _L, _L, _P, _P, _I, _P, _P, _P]),
+    "sirius_attn_paged": (_I, [_P, _I, _L, _P, _I, _F, _F, _P, _I, _P, _P, _P, _Z, _P]),
     "sirius_rmsnorm": (_I, [_P, _I, _I, _F, _P, _P]),
     "sirius_fill_normal_bf16": (_I, [_P, _Z, ctypes.c_uint64, _F, _F, _P]),
     "sirius_profile_enable": (_I, [_I]),
@@ -693,6 +695,37 @@ def sirius_kv_append(q, k, v, k_pages, v_pages, page_table, cache_pos, freqs=Non
     _check(lib().sirius_kv_append(_ptr(q), qt, ldq, _ptr(k), _ptr(v), _dtype(k), ldk, ldv, ctypes.byref(cache),
                                   _ptr(positions), h, ctypes.byref(rot), _ptr(q_out), _handle()))
     return q_out
+
+
+def sirius_attn_paged(q, k_pages, v_pages, page_table, cache_pos, *, tok_start=None, max_n=None, scale=0.0, softcap=0.0,
+                      slopes=None, window=0, mask=None, out=None, ws=None, stream=None):
+    """q [T, H, hd] (fp32 or bf16, tokens may be apart) over the cache that sirius_kv_append fills, after the
+    append and before cache_pos moves. tok_start [B + 1] int32 or None (T / B tokens each); max_n: the most
+    tokens of a sequence (with tok_start, T unless given). slopes [H] fp32, mask [T] int64 words of chunk
+    bits. Returns out [T, H, hd] of q's type."""
+    if stream is not None:
+        return _on(stream, sirius_attn_paged, locals())
+    if _elsewhere(q):
+        return _there(q, sirius_attn_paged, locals())
+    torch = _torch()
+    t, h, hd, ldq = _rows(q, "q")
+    qt = _dtype(q)
+    if out is None:
+        out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
+    _need(out.dtype is q.dtype and out.shape == q.shape and out.is_contiguous(), "out must be like q, contiguous")
+    if slopes is not None:
+        _need(slopes.dtype is torch.float32 and tuple(slopes.shape) == (h,) and slopes.is_contiguous(),
+              "slopes must be fp32 [H], contiguous")
+    if mask is not None:
+        _need(mask.dtype is torch.int64 and tuple(mask.shape) == (t,) and mask.is_contiguous(),
+              "mask must be int64 [T], contiguous")
+    _same_device(q, k_pages, v_pages, page_table, cache_pos, tok_start, slopes, mask, out, ws)
+    cache = _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n)
+    if ws is None:
+        ws = workspace(OP_ATTN_PAGED, cache.B, cache.max_n, h * 65536 + cache.n_kv_heads, hd, device=q.device)
+    _check(lib().sirius_attn_paged(_ptr(q), qt, ldq, ctypes.byref(cache), h, scale, softcap, _ptr(slopes), window,
+                                   _ptr(mask), _ptr(out), _ptr(ws), ws.numel(), _handle()))
+    return out
 
 
 def sirius_rmsnorm(h, eps=1e-5, *, out=None, stream=None):

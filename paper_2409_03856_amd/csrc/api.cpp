@@ -221,6 +221,13 @@ size_t sirius_workspace_size(int op, int B, int d_model, int d_ff, int T_or_V, i
         return 0;
       return sirius::attn_layout(std::max(B, 1), d_model, H, Hkv, T_or_V, K_or_R).total;
     }
+    case SIRIUS_OP_ATTN_PAGED: {
+      const int H = d_ff >> 16, Hkv = d_ff & 0xffff;
+      if (B < 0 || d_model < 0 || d_model > kMaxCacheLen || H < 1 || Hkv < 1 || H % Hkv != 0 || T_or_V < 8 ||
+          T_or_V > 128 || T_or_V % 8 != 0 || (long)H / Hkv * d_model > INT32_MAX)
+        return 0;
+      return sirius::paged_attn_layout(B, d_model, H, Hkv, T_or_V).total;
+    }
     case SIRIUS_OP_TREE_BUILD:
       if (B < 0 || d_model < 1 || d_model > kMaxTreeBuildW || d_ff < 1 || d_ff > kMaxTreeBuildW ||
           T_or_V < 1 || (long)d_model * T_or_V < d_ff)

@@ -1,0 +1,718 @@
+// Attention over the paged cache, on gfx950.
+//
+// Token i of sequence b stands at cache row p + i (p = cache_pos[b]); its H query heads read key/value
+// head h / G (G = H / Hkv) of rows 0 .. p + i, less what a window or a mask of the chunk hides:
+//   s_j = scale q . k_j, capped (cap tanh(s / cap)), less slope (p + i - j);  out = sum_j softmax(s)_j v_j.
+// The G n query rows of a sequence that share a key/value head (r = i G + h % G) are processed together.
+//
+// The rows of a call are cut into units (a sequence, a range of its visible rows) on the device, where
+// the lengths are: units are as long as makes about kTargetWgs workgroups of equal work, so ragged
+// batches stay balanced. A sequence of one unit is written out directly; the others leave (max, sum,
+// output) per unit and row, and attn_paged_merge_kernel joins them in order.
+//
+// attn_rows_kernel: up to 16 QT query rows per workgroup, four waves that take every fourth tile of
+// 32 positions each and are merged at the end. Scores are K Q^T on the matrix units, whose result (a lane
+// holds one query row and, by the order in which key rows are dealt to the operand's rows, eight
+// consecutive positions) is the operand of V^T P^T as it is. Keys lie row by row and values column by
+// column in the cache, so that both operands are 16-byte loads straight into registers: no LDS, no
+// barrier in the loop, one tile ahead in flight. fp32 queries and their probabilities go in as three
+// bf16 pieces that hold every bit; bf16 ones in one piece and probabilities in two.
+#include <float.h>
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+#include "paged.h"
+#include "profile.h"
+
+namespace sirius {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kTile = 32;           // positions per wave step
+constexpr int kStep = kTile * kWaves;
+constexpr int kTargetWgs = 512;     // workgroups wanted: two per CU
+constexpr int kMaxUnits = 256;      // ranges that the whole call is cut into at most, besides whole sequences
+constexpr int kGroups = 512;        // 8-position groups whose pages are staged at a time
+
+struct Args {
+  PagedView pg;
+  const void* q;
+  long ldq;
+  int H, Hkv, hd, G, rgroups, units;  // units: ranges wanted (1: every sequence whole)
+  float scale, cap;
+  const float* slopes;
+  int window;
+  const uint64_t* mask;
+  void* out;
+  float* pm;
+  float* pl;
+  float* po;
+  int2* info;  // [B]: first slot of the partials, units
+};
+
+__device__ __forceinline__ uint32_t high_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float rest(float x) {  // less its truncation to bf16; 0 for infinities
+  const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  return h == x ? 0.f : x - h;
+}
+__device__ __forceinline__ float rest_finite(float x) {
+  return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+}
+
+// e^x for x <= 0 to about one ulp: exp2 of the rounded x log2(e), times the first order of what the
+// rounding left off. Below -200 (hidden: -inf) 0; a NaN stays one.
+__device__ __forceinline__ float exp_neg(float x) {
+  constexpr float kHi = 1.44269502162933349609375f, kLo = 1.9259629911e-8f, kLn2 = 0.693147180559945f;
+  x = __builtin_elementwise_maximum(x, -200.f);
+  const float t = x * kHi;
+  const float d = fmaf(x, kLo, fmaf(x, kHi, -t));
+  return __builtin_amdgcn_exp2f(t) * fmaf(d, kLn2, 1.f);
+}
+
+// cap tanh(x / cap): the series of tanh up to 0.35 (the next term is 1e-8 of it), beyond it
+// 1 - 2 / (e^2a + 1).
+__device__ __forceinline__ float capped(float x, float cap, float inv) {
+  const float y = x * inv, a = fabsf(y), z = y * y;
+  float t = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -8.86323553e-3f, 2.18694885e-2f), -5.39682540e-2f), 0.133333333f), -0.333333333f), 1.f);
+  if (a > 0.35f) t = copysignf(1.f - 2.f / (__builtin_amdgcn_exp2f(fminf(a, 40.f) * 2.88539008f) + 1.f), y);
+  return y == y ? cap * t : y;
+}
+
+// A workgroup's share: positions [c0, c1) of sequence b, whose first seen row is lo.
+struct Unit {
+  int b, c0, c1, lo, slot, count, part;  // unit `part` of the sequence's `count`; slot: of its first partial
+  int first, n, p;                 // its tokens, its position
+};
+
+// Rows that a sequence's tokens see: from the first token's window to the last token, from a tile's start.
+__device__ __forceinline__ int first_seen(const Args& a, int p) {
+  return a.window > 0 ? max(0, p + 1 - a.window) : 0;
+}
+__device__ __forceinline__ bool valid(const Args& a, int p, int n) { return n <= a.pg.n && rows_fit(a.pg, p, n); }
+
+__device__ __forceinline__ int span_of(const Args& a, int b) {
+  const int n = tokens_of(a.pg, b).y, p = a.pg.pos[b];
+  if (n == 0) return 0;
+  if (!valid(a, p, n)) return 1;
+  return p + n - (first_seen(a, p) & ~(kTile - 1));
+}
+
+__device__ __forceinline__ int wave_add(int v) {
+  for (int m = 1; m < kWave; m <<= 1) v += __shfl_xor(v, m, kWave);
+  return v;
+}
+
+// The unit with this number, b = -1 behind the last. Every workgroup counts for itself: one sequence
+// per thread, the total of the visible rows first, then the units before.
+__device__ __forceinline__ Unit find_unit(const Args& a, int number) {
+  __shared__ int s_w[2][kWaves];
+  __shared__ int s_hit[5];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int B = a.pg.B;
+  Unit u{};
+  int length = 1 << 30;  // rows per unit
+  if (a.units <= 1) {
+    u.b = number < B ? number : -1;
+    u.count = 1;
+  } else {
+    long total = 0;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+      // spans are at most 2^20: a block's sum fits an int
+      const int s = wave_add(b0 + tid < B ? span_of(a, b0 + tid) : 0);
+      if (lane == 0) s_w[0][wave] = s;
+      __syncthreads();
+      total += (long)s_w[0][0] + s_w[0][1] + s_w[0][2] + s_w[0][3];
+      __syncthreads();
+    }
+    length = (int)max((total + a.units - 1) / a.units, 1l);
+    length = (length + kStep - 1) / kStep * kStep;
+    int before = 0, slots = 0;  // units and partial slots before this block
+    if (tid == 0) s_hit[0] = -1;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+      const int s = b0 + tid < B ? span_of(a, b0 + tid) : 0;
+      const int cnt = (s + length - 1) / length, sl = cnt > 1 ? cnt : 0;
+      int ic = cnt, is = sl;
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int c = __shfl_up(ic, o, kWave), d = __shfl_up(is, o, kWave);
+        if (lane >= o) {
+          ic += c;
+          is += d;
+        }
+      }
+      if (lane == kWave - 1) {
+        s_w[0][wave] = ic;
+        s_w[1][wave] = is;
+      }
+      __syncthreads();
+      int ec = before + ic - cnt, es = slots + is - sl;
+      for (int w = 0; w < wave; ++w) {
+        ec += s_w[0][w];
+        es += s_w[1][w];
+      }
+      if (number >= ec && number < ec + cnt) {
+        s_hit[0] = b0 + tid;
+        s_hit[1] = number - ec;
+        s_hit[2] = cnt;
+        s_hit[3] = es;
+        s_hit[4] = s;
+      }
+      before += s_w[0][0] + s_w[0][1] + s_w[0][2] + s_w[0][3];
+      slots += s_w[1][0] + s_w[1][1] + s_w[1][2] + s_w[1][3];
+      __syncthreads();
+      if (number < before) break;
+    }
+    u.b = s_hit[0];
+    if (u.b < 0) return u;
+    u.count = s_hit[2];
+    u.slot = s_hit[3];
+    length = (s_hit[4] + u.count - 1) / u.count;
+    length = (length + kStep - 1) / kStep * kStep;
+  }
+  if (u.b < 0) return u;
+  const int2 tk = tokens_of(a.pg, u.b);
+  u.first = tk.x;
+  u.n = tk.y;
+  u.p = a.pg.pos[u.b];
+  u.lo = first_seen(a, u.p);
+  if (u.n == 0 && a.units <= 1) {
+    u.b = -1;
+    return u;
+  }
+  if (!valid(a, u.p, u.n)) return u;  // c0 = c1
+  const int base = u.lo & ~(kTile - 1);
+  u.part = a.units <= 1 ? 0 : s_hit[1];
+  u.c0 = (int)min((long)base + (long)u.part * length, (long)u.p + u.n);
+  u.c1 = (int)min((long)u.c0 + length, (long)u.p + u.n);
+  return u;
+}
+
+__device__ __forceinline__ void put(float* p, float f) { *p = f; }
+__device__ __forceinline__ void put(uint16_t* p, float f) { *p = __builtin_bit_cast(uint16_t, (__bf16)f); }
+__device__ __forceinline__ void put4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void put4(uint16_t* p, float4 v) {
+  uint2 w;
+  w.x = __builtin_bit_cast(uint16_t, (__bf16)v.x) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v.y) << 16;
+  w.y = __builtin_bit_cast(uint16_t, (__bf16)v.z) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v.w) << 16;
+  *reinterpret_cast<uint2*>(p) = w;
+}
+__device__ __forceinline__ float value_at(const float* p, int i) { return p[i]; }
+__device__ __forceinline__ float value_at(const uint16_t* p, int i) { return bf16_lo(p[i]); }
+
+// What a query row sees.
+struct RowLimits {
+  int low, last, p;  // rows low .. last, of those from p on the ones whose bit is set
+  uint64_t bits;
+  __device__ __forceinline__ bool sees(int pos) const {
+    return pos >= low && pos <= last && (pos < p || ((bits >> (pos - p)) & 1) != 0);
+  }
+};
+template <bool MOD>
+__device__ __forceinline__ RowLimits limits(const Args& a, const Unit& u, int r, int nrows) {
+  RowLimits l{0, -1, 0x7fffffff, 0};
+  if (r < nrows) {
+    const int i = r / a.G;
+    l.last = u.p + i;
+    if (MOD) {
+      if (a.window > 0) l.low = max(0, u.p + i + 1 - a.window);
+      if (a.mask != nullptr) {
+        l.p = u.p;
+        l.bits = a.mask[u.first + i];
+      }
+    }
+  }
+  return l;
+}
+
+// One query row over the unit's positions in plain fp32 products, by one wave: what the matrix units'
+// pieces make NaN of (an infinite key or value times a zero piece; a hidden row's infinity times a zero
+// probability) although the formula does not.
+template <typename TQ>
+__device__ __forceinline__ void whole_row(const Args& a, const Unit& u, int r, int kvh, float* po, float* pm, float* pl) {
+  const int lane = threadIdx.x & (kWave - 1), hd = a.hd, ps = a.pg.page_size;
+  const int i = r / a.G, h = kvh * a.G + (r - i * a.G);
+  const TQ* q = static_cast<const TQ*>(a.q) + (long)(u.first + i) * a.ldq + (long)h * hd;
+  const RowLimits lim = limits<true>(a, u, r, 0x7fffffff);
+  auto place = [&](int pos, int& off) {
+    const int pg = page_of(a.pg, pos);
+    off = pos - pg * ps;
+    return (long)a.pg.table[(size_t)u.b * a.pg.max_pages + pg] * a.Hkv + kvh;
+  };
+  auto score = [&](int pos) {
+    int off;
+    const uint16_t* k = a.pg.k_pages + (place(pos, off) * ps + off) * hd;
+    float s = 0.f;
+    for (int c = 0; c < hd; ++c) s = fmaf(value_at(q, c), bf16_lo(k[c]), s);
+    s *= a.scale;
+    if (a.cap > 0.f) s = capped(s, a.cap, 1.f / a.cap);
+    if (a.slopes != nullptr) s -= a.slopes[h] * (float)(u.p + i - pos);
+    return s;
+  };
+  float m = -INFINITY;
+  for (int pos = u.c0 + lane; pos < u.c1; pos += kWave)
+    if (lim.sees(pos)) m = fmaxf(m, score(pos));
+  for (int k = 1; k < kWave; k <<= 1) m = fmaxf(m, __shfl_xor(m, k, kWave));
+  float l = 0.f, o0 = 0.f, o1 = 0.f;  // columns lane and lane + 64
+  for (int base = u.c0; base < u.c1; base += kWave) {
+    float w = 0.f;
+    if (base + lane < u.c1 && lim.sees(base + lane)) {
+      const float s = score(base + lane);
+      w = s == -INFINITY ? 0.f : expf(s - m);
+    }
+    l += w;
+    for (int j = 0; j < min(kWave, u.c1 - base); ++j) {
+      const float wj = __shfl(w, j, kWave);
+      if (!lim.sees(base + j) || wj == 0.f) continue;
+      int off;
+      const uint16_t* v = a.pg.v_pages + place(base + j, off) * hd * ps + off;
+      if (lane < hd) o0 = fmaf(wj, bf16_lo(v[(long)lane * ps]), o0);
+      if (lane + kWave < hd) o1 = fmaf(wj, bf16_lo(v[(long)(lane + kWave) * ps]), o1);
+    }
+  }
+  l = wave_sum(l);
+  if (po != nullptr) {
+    if (lane < hd) po[lane] = o0;
+    if (lane + kWave < hd) po[lane + kWave] = o1;
+    if (lane == 0) {
+      *pm = m;
+      *pl = l;
+    }
+  } else {
+    TQ* out = static_cast<TQ*>(a.out) + ((long)(u.first + i) * a.H + h) * hd;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (lane < hd) put(out + lane, l == 0.f ? 0.f : o0 * inv);
+    if (lane + kWave < hd) put(out + lane + kWave, l == 0.f ? 0.f : o1 * inv);
+  }
+}
+
+// A sequence outside its table, or a page outside the pool: NaN for its rows of this head.
+template <typename TQ>
+__device__ __forceinline__ void not_a_number(const Args& a, const Unit& u, int kvh, int r0, int r1, int R) {
+  const int tid = threadIdx.x;
+  if (u.count > 1) {
+    for (int r = r0 + tid; r < r1; r += kThreads) {
+      const size_t row = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R + r;
+      a.pm[row] = 0.f;
+      a.pl[row] = __builtin_nanf("");
+    }
+    return;
+  }
+  for (int e = tid; e < (r1 - r0) * a.hd; e += kThreads) {
+    const int r = r0 + e / a.hd, i = r / a.G, h = kvh * a.G + (r - i * a.G);
+    put(static_cast<TQ*>(a.out) + ((long)(u.first + i) * a.H + h) * a.hd + e % a.hd, __builtin_nanf(""));
+  }
+}
+
+// KS: 32-wide steps of the head size. QT: 16-row query tiles. MOD: any of cap, slopes, window, mask.
+template <typename TQ, int KS, int QT, bool MOD>
+__global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
+  constexpr bool kF32 = sizeof(TQ) == 4;
+  constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : 2;  // pieces of queries and probabilities
+  constexpr int kHd = KS * 32, DT = KS * 2;
+  __shared__ uint2 s_page[kGroups];  // page, offset of an 8-position group
+  __shared__ int s_bad, s_nan;
+  __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][kHd + 4];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int fr = lane & 15, g = lane >> 4, hd8 = a.hd >> 3, ps = a.pg.page_size;
+  // heads fastest: workgroups of one head run on one XCD where there are 8 of them
+  const int kvh = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv % a.rgroups;
+  const Unit u = find_unit(a, blockIdx.x / (a.Hkv * a.rgroups));
+  if (u.b < 0) return;
+  const int R = a.G * a.pg.n, r0 = rg * 16 * QT, nrows = u.n * a.G;
+  if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
+  if (u.c1 <= u.c0 && !valid(a, u.p, u.n)) {
+    // every row, also those behind the row groups that the call was launched for
+    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, nrows, R);
+    return;
+  }
+  if (r0 >= nrows) return;
+  const int nr = min(16 * QT, nrows - r0);
+  const size_t prow = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R + r0;  // this unit's partial rows
+  // positions that the group's rows see at all
+  const int last = u.p + (r0 + nr - 1) / a.G;
+  const int c1 = min(u.c1, last + 1);
+  // ---- queries: the B operand, lane (row, 8 columns of each step)
+  bf16x8_t qf[QT][KS][NQ];
+  RowLimits lim[QT];
+  float slope[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = r0 + 16 * t + fr, i = r / a.G, h = kvh * a.G + (r - i * a.G);
+    const bool there = r < nrows;
+    lim[t] = limits<MOD>(a, u, r, nrows);
+    slope[t] = MOD && a.slopes != nullptr && there ? a.slopes[h] : 0.f;
+    const TQ* src = static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int c = 4 * s + g;
+      const bool on = there && c < hd8;
+      if constexpr (kF32) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (on) {
+          const float4 x = *reinterpret_cast<const float4*>(src + 8 * c), y = *reinterpret_cast<const float4*>(src + 8 * c + 4);
+          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        }
+#pragma unroll
+        for (int pc = 0; pc < 3; ++pc) {
+          qf[t][s][pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]),
+                                                                  high_halves(v[4], v[5]), high_halves(v[6], v[7])));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
+        }
+      } else {
+        qf[t][s][0] = __builtin_bit_cast(bf16x8_t, on ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u));
+      }
+    }
+  }
+  float m[QT], l[QT];
+  floatx4_t o[QT][DT];  // columns 16 d + 4 g + e of row fr
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -FLT_MAX;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
+  const int low_last = MOD && a.window > 0 ? max(0, last + 1 - a.window) : 0;  // below it some row sees nothing
+  if (tid == 0) s_bad = s_nan = 0;
+
+  struct Frag {
+    uint4 k[2][KS];
+    uint4 v[DT];
+  };
+  auto load = [&](Frag& f, int t0, int seg) {  // the tile at t0; groups are staged from position seg
+    const int gk = (lane >> 2) & 3;
+    const uint2 pk = s_page[((t0 - seg) >> 3) + gk], pv = s_page[((t0 - seg) >> 3) + g];
+    const uint4* kp = reinterpret_cast<const uint4*>(a.pg.k_pages) +
+                      (((size_t)pk.x * a.Hkv + kvh) * ps + pk.y + (lane & 3)) * hd8 + g;
+    const uint4* vp = reinterpret_cast<const uint4*>(a.pg.v_pages + (((size_t)pv.x * a.Hkv + kvh) * a.hd + fr) * ps + pv.y);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        f.k[t][s] = 4 * s + g < hd8 ? kp[4 * t * hd8 + 4 * s] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      f.v[d] = 16 * d + fr < a.hd ? vp[(size_t)16 * d * (ps >> 3)] : make_uint4(0u, 0u, 0u, 0u);
+  };
+  auto compute = [&](Frag& f, int t0) {
+    if (t0 + kTile > c1) {  // uniform: nothing of the rows behind reaches the sums
+      uint32_t keep[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int pos = t0 + 8 * g + 2 * e;
+        keep[e] = (pos < c1 ? 0xffffu : 0u) | (pos + 1 < c1 ? 0xffff0000u : 0u);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        f.v[d] = make_uint4(f.v[d].x & keep[0], f.v[d].y & keep[1], f.v[d].z & keep[2], f.v[d].w & keep[3]);
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float x[8];  // positions t0 + 8 g + e
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        floatx4_t hi = floatx4_t{0.f, 0.f, 0.f, 0.f}, low = hi;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, f.k[h][s]);
+#pragma unroll
+          for (int pc = NQ - 1; pc > 0; --pc) low = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][pc], low, 0, 0, 0);
+          hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][0], hi, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * h + e] = kF32 ? hi[e] + low[e] : hi[e];
+      }
+      if constexpr (MOD || kF32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= a.scale;
+      }
+      if constexpr (MOD) {
+        if (a.cap > 0.f) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = capped(x[e], a.cap, inv_cap);
+        }
+        if (a.slopes != nullptr) {
+          const float away = (float)(lim[t].last - t0 - 8 * g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = fmaf(-slope[t], away - (float)e, x[e]);
+        }
+      }
+      // uniform: some row does not see all of it (a mask may hide row p from its own token)
+      if (t0 + kTile > min(c1, MOD ? u.p : u.p + 1) || (MOD && t0 < low_last)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int pos = t0 + 8 * g + e;
+          const bool seen = MOD ? lim[t].sees(pos) : pos <= lim[t].last;
+          if (!seen || pos >= c1) x[e] = -INFINITY;
+        }
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float m_new = fmaxf(m[t], mx);
+      float alpha, pr[8], sum = 0.f;
+      if constexpr (kF32) {
+        alpha = exp_neg(m[t] - m_new);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = exp_neg(x[e] - m_new);
+      } else {
+        const float c = MOD ? 1.44269504088896341f : to_exp2;
+        alpha = __builtin_amdgcn_exp2f((m[t] - m_new) * c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f((x[e] - m_new) * c);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += pr[e];
+      m[t] = m_new;
+      l[t] = fmaf(l[t], alpha, sum);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+      bf16x8_t pf[NP];
+#pragma unroll
+      for (int pc = 0; pc < NP; ++pc) {
+        pf[pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(pr[0], pr[1]), high_halves(pr[2], pr[3]),
+                                                         high_halves(pr[4], pr[5]), high_halves(pr[6], pr[7])));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = rest_finite(pr[e]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int pc = NP - 1; pc >= 0; --pc)
+          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f.v[d]), pf[pc], o[t][d], 0, 0, 0);
+    }
+  };
+  for (int seg = u.c0; seg < c1; seg += kGroups * 8) {
+    const int end = min(c1, seg + kGroups * 8);
+    __syncthreads();  // the pages staged before are read
+    for (int e = tid; e < kGroups && seg + 8 * e < end + kStep; e += kThreads) {
+      const int pos = seg + 8 * e;
+      uint2 w = make_uint2(0u, 0u);
+      if (pos < c1) {
+        const int pg = page_of(a.pg, pos), id = a.pg.table[(size_t)u.b * a.pg.max_pages + pg];
+        if (id >= 0 && id < a.pg.n_pages) w = make_uint2((uint32_t)id, (uint32_t)(pos - pg * ps));
+        else if (pos + 8 > u.lo) s_bad = 1;
+      }
+      s_page[e] = w;
+    }
+    __syncthreads();
+    Frag fa, fb;
+    int t0 = seg + kTile * wave;
+    if (t0 < end) load(fa, t0, seg);
+    for (; t0 < end; t0 += 2 * kStep) {
+      if (t0 + kStep < end) load(fb, t0 + kStep, seg);
+      compute(fa, t0);
+      if (t0 + kStep >= end) break;
+      if (t0 + 2 * kStep < end) load(fa, t0 + 2 * kStep, seg);
+      compute(fb, t0 + kStep);
+    }
+  }
+  // ---- the waves' shares joined in order, one query tile at a time
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] += __shfl_xor(l[t], 16, kWave);
+    l[t] += __shfl_xor(l[t], 32, kWave);
+    floatx4_t chk = floatx4_t{l[t], 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DT; ++d) chk += o[t][d];
+    const float c = (chk[0] + chk[1]) + (chk[2] + chk[3]);
+    // infinite sums count: they may be an overflow's, or an infinite value's, which the pieces turned
+    if (__ballot(!(fabsf(c) < INFINITY)) != 0 && lane == 0) s_nan = 1;
+  }
+  __syncthreads();
+  if (s_bad) {
+    not_a_number<TQ>(a, u, kvh, r0, r0 + nr, R);
+    return;
+  }
+  if (s_nan) {
+    Unit w = u;
+    w.c1 = c1;
+    for (int r = wave; r < nr; r += kWaves)
+      whole_row<TQ>(a, w, r0 + r, kvh, u.count > 1 ? a.po + (prow + r) * a.hd : nullptr, a.pm + prow + r, a.pl + prow + r);
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    if (t > 0) __syncthreads();
+    if (g == 0) {
+      s_m[wave][fr] = l[t] > 0.f ? m[t] : -INFINITY;
+      s_l[wave][fr] = l[t];
+    }
+    __syncthreads();
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][fr]);
+    const float unit = kF32 || MOD ? 1.f : a.scale;  // m counts unscaled scores there
+    const float f = l[t] > 0.f ? expf((m[t] - M) * unit) : 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+      *reinterpret_cast<float4*>(&s_o[wave][fr][16 * d + 4 * g]) =
+          make_float4(o[t][d][0] * f, o[t][d][1] * f, o[t][d][2] * f, o[t][d][3] * f);
+    __syncthreads();
+    const int rows = min(16, nr - 16 * t);
+    for (int e = tid; e < rows * (kHd / 4); e += kThreads) {
+      const int rr = e / (kHd / 4), c = 4 * (e % (kHd / 4));
+      if (c >= a.hd) continue;
+      float Mr = -INFINITY, lt = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) Mr = fmaxf(Mr, s_m[w][rr]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(&s_o[w][rr][c]);
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        const float mw = s_m[w][rr];
+        lt += mw > -INFINITY ? s_l[w][rr] * expf((mw - Mr) * unit) : 0.f;
+      }
+      const int r = r0 + 16 * t + rr;
+      if (u.count > 1) {
+        const size_t row = prow + 16 * t + rr;
+        *reinterpret_cast<float4*>(a.po + row * a.hd + c) = v;
+        if (c == 0) {
+          a.pm[row] = Mr * (Mr > -INFINITY ? unit : 1.f);
+          a.pl[row] = lt;
+        }
+      } else {
+        const int i = r / a.G, h = kvh * a.G + (r - i * a.G);
+        if (lt == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);
+        else v = make_float4(v.x / lt, v.y / lt, v.z / lt, v.w / lt);
+        put4(static_cast<TQ*>(a.out) + ((long)(u.first + i) * a.H + h) * a.hd + c, v);
+      }
+    }
+  }
+}
+
+// The units of a sequence joined in order: one wave per token and head.
+template <typename TQ>
+__global__ __launch_bounds__(kThreads) void attn_paged_merge_kernel(Args a) {
+  constexpr int kAhead = 8;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+  const int t = blockIdx.x, h = blockIdx.y * kWaves + wave;
+  if (h >= a.H) return;
+  const int b = sequence_of_wave(a.pg, t);
+  if (b < 0) return;
+  const int2 tk = tokens_of(a.pg, b);
+  if (t < tk.x || t >= tk.x + min(tk.y, a.pg.n)) return;
+  const int2 info = a.info[b];
+  if (info.y <= 1) return;
+  const int R = a.G * a.pg.n, kvh = h / a.G, r = (t - tk.x) * a.G + (h - kvh * a.G);
+  const size_t row0 = ((size_t)info.x * a.Hkv + kvh) * R + r, stride = (size_t)a.Hkv * R;
+  float M = -INFINITY;
+  for (int s = lane; s < info.y; s += kWave) M = fmaxf(M, a.pm[row0 + s * stride]);
+  for (int k = 1; k < kWave; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, kWave));
+  const int c = 2 * lane;
+  float den = 0.f;
+  float2 num = make_float2(0.f, 0.f);
+  for (int s0 = 0; s0 < info.y; s0 += kWave) {
+    const int ns = min(kWave, info.y - s0);
+    float w = 0.f;
+    if (lane < ns) {
+      const size_t row = row0 + (s0 + lane) * stride;
+      const float ms = a.pm[row];
+      w = ms > -INFINITY ? expf(ms - M) : 0.f;
+      den += w > 0.f || a.pl[row] != a.pl[row] ? a.pl[row] * w : 0.f;
+    }
+    for (int s = 0; s < ns; s += kAhead) {
+      float2 x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        x[k] = s + k < ns && c < a.hd ? *reinterpret_cast<const float2*>(a.po + (row0 + (s0 + s + k) * stride) * a.hd + c)
+                                      : make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float wk = __shfl(w, (s + k) & (kWave - 1), kWave);
+        if (s + k < ns && wk > 0.f) {  // an empty unit's outputs were not written
+          num.x = fmaf(wk, x[k].x, num.x);
+          num.y = fmaf(wk, x[k].y, num.y);
+        }
+      }
+    }
+  }
+  den = wave_sum(den);
+  if (c < a.hd) {
+    TQ* out = static_cast<TQ*>(a.out) + ((long)t * a.H + h) * a.hd + c;
+    put(out, den == 0.f ? 0.f : num.x / den);
+    put(out + 1, den == 0.f ? 0.f : num.y / den);
+  }
+}
+
+int tiles_of(int rows) { return rows <= 16 ? 1 : 2; }  // query tiles of a workgroup
+
+}  // namespace
+
+PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd) {
+  PagedAttnLayout L{};
+  const int R = H / Hkv * n;
+  L.rgroups = ceil_div(std::max(R, 1), 16 * tiles_of(R));
+  const long wgs = (long)Hkv * L.rgroups;
+  L.units = (int)std::min<long>((kTargetWgs + wgs - 1) / wgs, kMaxUnits);
+  // A unit is at least the average row count over `units`: sequences of more than one unit make fewer
+  // than 2 units of them.
+  const size_t rows = L.units > 1 ? (size_t)2 * L.units * Hkv * R : 0;
+  Carve c;
+  L.info = c.take((size_t)std::max(B, 1) * sizeof(int2));
+  L.pm = c.take(rows * sizeof(float));
+  L.pl = c.take(rows * sizeof(float));
+  L.po = c.take(rows * hd * sizeof(float));
+  L.total = c.off;
+  return L;
+}
+
+hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* ws, const PagedAttnLayout& L,
+                             hipStream_t stream) {
+  Args a{};
+  a.pg = pg;
+  a.q = c.q; a.ldq = c.ldq;
+  a.H = c.H; a.Hkv = c.Hkv; a.hd = c.hd; a.G = c.H / c.Hkv;
+  a.rgroups = L.rgroups; a.units = L.units;
+  a.scale = c.scale; a.cap = c.cap; a.slopes = c.slopes; a.window = c.window; a.mask = c.mask;
+  a.out = c.out;
+  a.info = reinterpret_cast<int2*>(ws + L.info);
+  a.pm = reinterpret_cast<float*>(ws + L.pm);
+  a.pl = reinterpret_cast<float*>(ws + L.pl);
+  a.po = reinterpret_cast<float*>(ws + L.po);
+  const bool mod = c.cap > 0.f || c.slopes != nullptr || c.window > 0 || c.mask != nullptr;
+  const int R = a.G * pg.n, qt = tiles_of(R), ks = ceil_div(c.hd, 32);
+  // every sequence has a unit, and the cuts add fewer than `units`
+  const long grid = (long)c.Hkv * L.rgroups * (pg.B + (L.units > 1 ? L.units : 0));
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  {
+    ProfScope prof("attn_paged", stream);
+#define SIRIUS_ROWS(TQ, KS, QT)                                                                     \
+  (mod ? klaunch(attn_rows_kernel<TQ, KS, QT, true>, (int)grid, kThreads, 0, stream, a)                  \
+       : klaunch(attn_rows_kernel<TQ, KS, QT, false>, (int)grid, kThreads, 0, stream, a))
+#define SIRIUS_ROWS_KS(TQ, QT)                                                                      \
+  (ks <= 2 ? SIRIUS_ROWS(TQ, 2, QT) : ks == 3 ? SIRIUS_ROWS(TQ, 3, QT) : SIRIUS_ROWS(TQ, 4, QT))
+    if (c.q_bf16) {
+      if (qt == 1) SIRIUS_ROWS_KS(uint16_t, 1);
+      else SIRIUS_ROWS_KS(uint16_t, 2);
+    } else {
+      if (qt == 1) SIRIUS_ROWS_KS(float, 1);
+      else SIRIUS_ROWS_KS(float, 2);
+    }
+#undef SIRIUS_ROWS_KS
+#undef SIRIUS_ROWS
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  // a table that holds one unit's rows at most is never cut
+  if (L.units <= 1 || (long)pg.max_pages * pg.page_size <= kStep) return hipSuccess;
+  ProfScope prof("attn_paged_merge", stream);
+  const dim3 mgrid(pg.T, ceil_div(c.H, kWaves));
+  if (c.q_bf16) klaunch(attn_paged_merge_kernel<uint16_t>, mgrid, kThreads, 0, stream, a);
+  else klaunch(attn_paged_merge_kernel<float>, mgrid, kThreads, 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace sirius

@@ -248,6 +248,26 @@ struct RopeCall {
 hipError_t launch_rope(const RopeCall& c, hipStream_t stream);
 hipError_t launch_kv_append(const RopeCall& c, const PagedView& pg, hipStream_t stream);
 
+struct PagedAttnLayout {
+  int rgroups, units;               // query-row groups per kv head, ranges that the call is cut into
+  size_t info, pm, pl, po, total;   // where sequences' partials lie; per unit and row: max, sum, output
+};
+PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd);
+// q [T][H][hd] (token stride ldq), out [T][H][hd] of the same type; cap 0, slopes null, window 0, mask null: none.
+struct PagedAttnCall {
+  const void* q;
+  bool q_bf16;
+  long ldq;
+  int H, Hkv, hd;
+  float scale, cap;
+  const float* slopes;
+  int window;
+  const uint64_t* mask;
+  void* out;
+};
+hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* ws, const PagedAttnLayout& L,
+                             hipStream_t stream);
+
 // ---- small decoder and the generation loop (model.hip)
 // h[i] = E[tokens[i]] widened to fp32 (0 for an id outside [0, V)); d % 8 == 0.
 hipError_t launch_embed(const int32_t* tokens, int n, const uint16_t* E, int d, int V, float* out,

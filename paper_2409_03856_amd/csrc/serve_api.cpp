@@ -225,4 +225,40 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
   return hip_status(sirius::launch_kv_append(c, view(cache), static_cast<hipStream_t>(stream)), fn);
 }
 
+int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_paged* cache, int H, float scale,
+                      float softcap, const float* slopes, int window, const uint64_t* mask, void* out, void* ws,
+                      size_t ws_bytes, void* stream) {
+  const char* fn = "sirius_attn_paged";
+  int rc;
+  if ((rc = check_paged_sizes(fn, cache))) return rc;
+  const int hd = cache->head_dim, Hkv = cache->n_kv_heads;
+  if ((rc = check_dtype(fn, q_dtype, "q_dtype")) || (rc = check_heads(fn, H, "H"))) return rc;
+  if (H % Hkv != 0) return fail(SIRIUS_EINVAL, "%s: H=%d must be a multiple of n_kv_heads=%d", fn, H, Hkv);
+  if (!(scale >= 0.f) || std::isinf(scale)) return fail(SIRIUS_EINVAL, "%s: scale must be finite and >= 0", fn);
+  if (!(softcap >= 0.f) || std::isinf(softcap)) return fail(SIRIUS_EINVAL, "%s: softcap must be finite and >= 0", fn);
+  if (window < 0) return fail(SIRIUS_EINVAL, "%s: window=%d < 0", fn, window);
+  if (mask != nullptr && cache->max_n > 64) return fail(SIRIUS_EINVAL, "%s: a mask needs max_n=%d <= 64", fn, cache->max_n);
+  if (cache->T == 0 || cache->B == 0) return SIRIUS_OK;
+  if ((rc = check_paged_ptrs(fn, cache)) || (rc = check_rows(fn, q, "q", H, hd, ldq)) || (rc = check_ptr(fn, out, "out")) ||
+      (rc = check_ptr(fn, ws, "ws")))
+    return rc;
+  const int64_t rows = (int64_t)(H / Hkv) * cache->max_n;
+  if (rows > INT32_MAX / 256) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
+  const sirius::PagedAttnLayout L = sirius::paged_attn_layout(cache->B, cache->max_n, H, Hkv, hd);
+  if ((int64_t)Hkv * L.rgroups * (cache->B + L.units) > INT32_MAX) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
+  if (ws_bytes < L.total) return fail(SIRIUS_EWORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, L.total);
+  sirius::PagedAttnCall c{};
+  c.q = q;
+  c.q_bf16 = q_dtype == SIRIUS_BF16;
+  c.ldq = ldq;
+  c.H = H; c.Hkv = Hkv; c.hd = hd;
+  c.scale = scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)hd));
+  c.cap = softcap;
+  c.slopes = slopes;
+  c.window = window;
+  c.mask = mask;
+  c.out = out;
+  return hip_status(sirius::launch_attn_paged(c, view(cache), static_cast<char*>(ws), L, static_cast<hipStream_t>(stream)), fn);
+}
+
 }  // extern "C"

@@ -101,3 +101,28 @@ def test_binding_refusals(lib):
         lib.sirius_rope_freqs(0)
     with pytest.raises(lib.SiriusError):
         lib.sirius_rope_freqs(64, 0.5)
+
+
+def test_attention_refusals(lib):
+    L = lib.lib()
+    base = dict(q=FAKE, qt=0, ldq=256, cache=_paged(lib), H=4, scale=0.0, cap=0.0, slopes=None, window=0, mask=None, out=FAKE,
+                ws=FAKE, n=1 << 30)
+
+    def call(**kw):
+        a = base | kw
+        a["cache"] = None if a["cache"] is None else ctypes.byref(a["cache"])
+        return L.sirius_attn_paged(*a.values(), None)
+
+    for kw in (dict(q=None), dict(q=ODD), dict(out=None), dict(out=ODD), dict(ws=None), dict(qt=2), dict(ldq=248), dict(H=3), dict(H=0),
+               dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(cap=-1.0), dict(cap=NAN), dict(cap=INF), dict(window=-1),
+               dict(cache=None), dict(mask=FAKE, cache=_paged(lib, max_n=65, T=130))):
+        assert call(**kw) == -1, kw
+    for kw in BAD_CACHES:
+        assert call(cache=_paged(lib, **kw)) == -1, kw
+    assert call(n=16) == -2
+    for kw in (dict(T=0, B=0), dict(T=0, max_n=0), dict(T=0, tok_start=1 << 20)):
+        assert call(cache=_paged(lib, **kw), q=None) == 0, kw
+    size = lambda *a: L.sirius_workspace_size(10, *a)
+    assert size(2, 3, 4 * 65536 + 2, 64, 0) > 0 and size(0, 0, 4 * 65536 + 2, 64, 0) > 0
+    for a in ((-1, 3, 4 * 65536 + 2, 64, 0), (2, -1, 4 * 65536 + 2, 64, 0), (2, 3, 3 * 65536 + 2, 64, 0), (2, 3, 4 * 65536 + 2, 60, 0)):
+        assert size(*a) == 0, a
