@@ -62,6 +62,7 @@ extern "C" {
 #define SIRIUS_OP_FFN_TOPK 8
 #define SIRIUS_OP_ATTN_KV 9
 #define SIRIUS_OP_ATTN_PAGED 10
+#define SIRIUS_OP_SAMPLE 11
 
 /*
  * Dense SwiGLU FFN (the full model, sparsity 0):
@@ -568,6 +569,36 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
                       const uint64_t* mask, void* out, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Sampling, where the other decisions here take the argmax (Algorithm 1 samples the corrected
+ * token): one token per row from given uniform numbers. With M the row's largest logit a token
+ * weighs w = exp((x - M) / T), 0 (dropped, not counted) where x is NaN or (x - M) / T < -700; with
+ * M = +inf the infinite logits weigh 1, the others 0. Of the tokens in the order (logit
+ * descending, index ascending) these stay, in turn:
+ *   the first k; of these the ones in front of which less than p times their mass lies; of these the
+ *   ones with w >= m; the best one always.
+ * The token is the first one in index order whose running kept mass exceeds u times the kept
+ * mass (u is clamped to [0, 1]; at 1 the last kept token of positive mass).
+ * Weights are formed in fp64 and added as whole numbers of 2^-(62 - ceil(log2 V)), so a call's
+ * result does not depend on the order of its sums.
+ *   logits [B, V] fp32, rows ld elements apart (ld >= V; 16-byte aligned base).
+ *   u      [B] fp32.
+ *   temperature [B] fp32 or NULL (1); 0 is greedy: the argmax, lowest index on ties.
+ *   top_k  [B] int32 or NULL; <= 0 or >= V: off.
+ *   top_p  [B] fp32 or NULL; >= 1: off; <= 0 keeps the best token.
+ *   min_p  [B] fp32 or NULL; <= 0: off; > 1 keeps the best token.
+ *   token  [B] int32 out; kept [B] int32 out or NULL: how many tokens stayed; prob [B] fp32 out or
+ *          NULL: the token's share of the kept mass.
+ * A row without a logit above -infinity, and one with a NaN parameter, a negative or an infinite
+ * temperature, gives token -1, kept 0, prob 0. Needs sirius_workspace_size(SIRIUS_OP_SAMPLE, ...).
+ * B == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null pointers (where not allowed above), B
+ * outside [0, 65535], V outside [1, 2^24], ld < V, misaligned logits; SIRIUS_EWORKSPACE.
+ */
+int sirius_sample(const float* logits, int64_t ld, int B, int V, const float* u,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, int32_t* token, int32_t* kept, float* prob, void* ws,
+                  size_t ws_bytes, void* stream);
+
+/*
  * RMSNorm with unit weight, the layer-stack glue around the FFN:
  *   out[b] = h[b] / sqrt(mean(h[b]^2) + eps). out may alias h.
  * Errors: SIRIUS_EINVAL for null pointers, d_model < 1, eps < 0.
@@ -606,7 +637,7 @@ int sirius_fill_normal_bf16(uint16_t* out, size_t n, uint64_t seed, float mean, 
  * "tree_topw", "tree_select"; "griffin_z", "griffin_rownorm", "griffin_score",
  * "griffin_topk", "condense"; "rmsnorm", "fill_normal"; "attn_partial",
  * "attn_combine", "kv_rollback"; "rope", "kv_append",
- * "attn_paged", "attn_paged_merge".
+ * "attn_paged", "attn_paged_merge"; "sample_row".
  * sirius_profile_reset drops every record (it waits for pending events).
  * Errors: SIRIUS_EINVAL for NULL arguments, SIRIUS_EHIP if an event fails.
  */
@@ -624,6 +655,7 @@ int sirius_profile_query(const char* kernel, double* total_ms, int64_t* launches
  *   TREE_VERIFY: B, K, W, V, bonus
  *   ATTN_KV: B, n, H * 65536 + Hkv, head_dim, Lmax
  *   ATTN_PAGED: B, max_n, H * 65536 + n_kv_heads, head_dim, unused
+ *   SAMPLE: B, unused, unused, V, unused
  * Returns 0 for an unknown op or invalid sizes. */
 size_t sirius_workspace_size(int op, int B, int d_model, int d_ff, int T_or_V, int K_or_R);
 

@@ -26,6 +26,7 @@ from ._lib import (  # noqa: F401
     sirius_rope,
     sirius_kv_append,
     sirius_attn_paged,
+    sirius_sample,
     sirius_rmsnorm,
     Model,
     sirius_model_workspace_size,
@@ -49,4 +50,5 @@ from ._lib import (  # noqa: F401
     OP_FFN_TOPK,
     OP_ATTN_KV,
     OP_ATTN_PAGED,
+    OP_SAMPLE,
 )

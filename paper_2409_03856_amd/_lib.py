@@ -35,6 +35,7 @@ OP_TREE_VERIFY = 7
 OP_FFN_TOPK = 8
 OP_ATTN_KV = 9
 OP_ATTN_PAGED = 10
+OP_SAMPLE = 11
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -64,6 +65,7 @@ SIGNATURES = {
     "sirius_rope": (_I, [_P, _I, _L, _P, _I, _L, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
     "sirius_kv_append": (_I, [_P, _I, _L, _P, _P, _I, _L, _L, _P, _P, _I, _P, _P, _P]),
     "sirius_attn_paged": (_I, [_P, _I, _L, _P, _I, _F, _F, _P, _I, _P, _P, _P, _Z, _P]),
+    "sirius_sample": (_I, [_P, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "sirius_rmsnorm": (_I, [_P, _I, _I, _F, _P, _P]),
     "sirius_fill_normal_bf16": (_I, [_P, _Z, ctypes.c_uint64, _F, _F, _P]),
     "sirius_profile_enable": (_I, [_I]),
@@ -726,6 +728,54 @@ def sirius_attn_paged(q, k_pages, v_pages, page_table, cache_pos, *, tok_start=N
     _check(lib().sirius_attn_paged(_ptr(q), qt, ldq, ctypes.byref(cache), h, scale, softcap, _ptr(slopes), window,
                                    _ptr(mask), _ptr(out), _ptr(ws), ws.numel(), _handle()))
     return out
+
+
+def _per_row(v, dtype, bsz, device, name):
+    """A parameter of sampling: None, a [B] tensor, or one value for every row."""
+    torch = _torch()
+    if v is None:
+        return None
+    if not isinstance(v, torch.Tensor):
+        return torch.full((bsz,), v, dtype=dtype, device=device)
+    _need(v.dtype is dtype and tuple(v.shape) == (bsz,) and v.is_contiguous(), f"{name} must be {dtype} [B], contiguous")
+    return v
+
+
+def sirius_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, token=None, kept=None, prob=None,
+                  ws=None, stream=None):
+    """logits [B, V] fp32 (rows may be apart), u [B] fp32 in [0, 1). temperature, top_p, min_p: fp32 [B]
+    or one number, top_k: int32 [B] or one number, None: off (temperature 1). Returns (token [B] int32, kept
+    [B] int32, prob [B] fp32)."""
+    if stream is not None:
+        return _on(stream, sirius_sample, locals())
+    if _elsewhere(logits):
+        return _there(logits, sirius_sample, locals())
+    torch = _torch()
+    _need(logits.dtype is torch.float32 and logits.dim() == 2, "logits must be fp32 [B, V]")
+    _need(logits.is_cuda, "tensors must live on the GPU")
+    bsz, vocab = logits.shape
+    _need(bsz == 0 or vocab <= 1 or logits.stride(1) == 1, "a row's logits must be contiguous")
+    ld = logits.stride(0) if bsz > 1 else vocab
+    dev = logits.device
+    f32, i32 = torch.float32, torch.int32
+    _need(u.dtype is f32 and tuple(u.shape) == (bsz,) and u.is_contiguous(), "u must be fp32 [B], contiguous")
+    temperature = _per_row(temperature, f32, bsz, dev, "temperature")
+    top_k, top_p = _per_row(top_k, i32, bsz, dev, "top_k"), _per_row(top_p, f32, bsz, dev, "top_p")
+    min_p = _per_row(min_p, f32, bsz, dev, "min_p")
+    if token is None:
+        token = torch.empty(bsz, dtype=i32, device=dev)
+    if kept is None:
+        kept = torch.empty(bsz, dtype=i32, device=dev)
+    if prob is None:
+        prob = torch.empty(bsz, dtype=f32, device=dev)
+    for t, d, n in ((token, i32, "token"), (kept, i32, "kept"), (prob, f32, "prob")):
+        _need(t.dtype is d and tuple(t.shape) == (bsz,) and t.is_contiguous(), f"{n} must be {d} [B], contiguous")
+    _same_device(logits, u, temperature, top_k, top_p, min_p, token, kept, prob, ws)
+    if ws is None:
+        ws = workspace(OP_SAMPLE, bsz, 0, 0, vocab, device=dev)
+    _check(lib().sirius_sample(_ptr(logits), ld, bsz, vocab, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                               _ptr(token), _ptr(kept), _ptr(prob), _ptr(ws), ws.numel(), _handle()))
+    return token, kept, prob
 
 
 def sirius_rmsnorm(h, eps=1e-5, *, out=None, stream=None):

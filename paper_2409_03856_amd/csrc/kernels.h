@@ -268,6 +268,26 @@ struct PagedAttnCall {
 hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* ws, const PagedAttnLayout& L,
                              hipStream_t stream);
 
+struct SampleLayout {
+  size_t total;
+};
+SampleLayout sample_layout(int B, int V);
+// logits [B][V] (row stride ld, 16-byte aligned base); the parameters [B] each, or null.
+struct SampleCall {
+  const float* logits;
+  long ld;
+  int B, V;
+  const float* u;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  int32_t* kept;
+  float* prob;
+};
+hipError_t launch_sample(const SampleCall& c, char* ws, const SampleLayout& L, hipStream_t stream);
+
 // ---- small decoder and the generation loop (model.hip)
 // h[i] = E[tokens[i]] widened to fp32 (0 for an id outside [0, V)); d % 8 == 0.
 hipError_t launch_embed(const int32_t* tokens, int n, const uint16_t* E, int d, int V, float* out,

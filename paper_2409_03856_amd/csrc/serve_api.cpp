@@ -261,4 +261,21 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
   return hip_status(sirius::launch_attn_paged(c, view(cache), static_cast<char*>(ws), L, static_cast<hipStream_t>(stream)), fn);
 }
 
+int sirius_sample(const float* logits, int64_t ld, int B, int V, const float* u, const float* temperature,
+                  const int32_t* top_k, const float* top_p, const float* min_p, int32_t* token, int32_t* kept, float* prob,
+                  void* ws, size_t ws_bytes, void* stream) {
+  const char* fn = "sirius_sample";
+  if (B < 0 || B > kMaxSeqs) return fail(SIRIUS_EINVAL, "%s: B=%d outside [0, %d]", fn, B, kMaxSeqs);
+  if (V < 1 || V > (1 << 24)) return fail(SIRIUS_EINVAL, "%s: V=%d outside [1, 2^24]", fn, V);
+  if (ld < V || ld > ((int64_t)1 << 31)) return fail(SIRIUS_EINVAL, "%s: rows of V=%d are %lld apart", fn, V, (long long)ld);
+  if (B == 0) return SIRIUS_OK;
+  int rc;
+  if ((rc = check_ptr(fn, logits, "logits")) || (rc = check_ptr(fn, ws, "ws"))) return rc;
+  if (u == nullptr || token == nullptr) return fail(SIRIUS_EINVAL, "%s: u or token is NULL", fn);
+  const sirius::SampleLayout L = sirius::sample_layout(B, V);
+  if (ws_bytes < L.total) return fail(SIRIUS_EWORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, L.total);
+  const sirius::SampleCall c{logits, (long)ld, B, V, u, temperature, top_k, top_p, min_p, token, kept, prob};
+  return hip_status(sirius::launch_sample(c, static_cast<char*>(ws), L, static_cast<hipStream_t>(stream)), fn);
+}
+
 }  // extern "C"

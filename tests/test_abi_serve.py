@@ -126,3 +126,22 @@ def test_attention_refusals(lib):
     assert size(2, 3, 4 * 65536 + 2, 64, 0) > 0 and size(0, 0, 4 * 65536 + 2, 64, 0) > 0
     for a in ((-1, 3, 4 * 65536 + 2, 64, 0), (2, -1, 4 * 65536 + 2, 64, 0), (2, 3, 3 * 65536 + 2, 64, 0), (2, 3, 4 * 65536 + 2, 60, 0)):
         assert size(*a) == 0, a
+
+
+def test_sampling_refusals(lib):
+    L = lib.lib()
+    base = dict(logits=FAKE, ld=100, B=2, V=100, u=FAKE, t=None, k=None, p=None, m=None, token=FAKE, kept=None, prob=None, ws=FAKE,
+                n=1 << 30)
+    call = lambda **kw: L.sirius_sample(*(base | kw).values(), None)
+    for kw in (dict(logits=None), dict(logits=ODD), dict(u=None), dict(token=None), dict(ws=None), dict(B=-1), dict(B=65536), dict(V=0),
+               dict(V=(1 << 24) + 1, ld=1 << 25), dict(ld=99), dict(ld=-1)):
+        assert call(**kw) == -1, kw
+    assert call(n=0) == -2
+    assert call(B=0, logits=None) == 0
+    assert L.sirius_workspace_size(11, 2, 0, 0, 100, 0) > 0 and L.sirius_workspace_size(11, 2, 0, 0, 0, 0) == 0
+    import torch
+    x = torch.zeros(2, 10)
+    with pytest.raises(ValueError, match="GPU"):
+        lib.sirius_sample(x, x[:, 0].contiguous())
+    with pytest.raises(ValueError, match="fp32"):
+        lib.sirius_sample(x.double(), x[:, 0].contiguous())
