@@ -20,6 +20,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 #include "paged.h"
@@ -309,9 +311,74 @@ __device__ __forceinline__ void not_a_number(const Args& a, const Unit& u, int k
   }
 }
 
-// KS: 32-wide steps of the head size. QT: 16-row query tiles. MOD: any of cap, slopes, window, mask.
-template <typename TQ, int KS, int QT, bool MOD>
+// A query row's operand: 8 columns of each 32-wide step, whole or in three pieces.
+template <typename TQ, int KS, int NQ>
+__device__ __forceinline__ void load_query(const TQ* src, bool there, int g, int hd8, bf16x8_t (&qf)[KS][NQ]) {
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int c = 4 * s + g;
+    const bool on = there && c < hd8;
+    if constexpr (NQ == 3) {
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (on) {
+        const float4 x = *reinterpret_cast<const float4*>(src + 8 * c), y = *reinterpret_cast<const float4*>(src + 8 * c + 4);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+      }
+#pragma unroll
+      for (int pc = 0; pc < 3; ++pc) {
+        qf[s][pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]),
+                                                             high_halves(v[4], v[5]), high_halves(v[6], v[7])));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
+      }
+    } else {
+      qf[s][0] = __builtin_bit_cast(bf16x8_t, on ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u));
+    }
+  }
+}
+
+// Probabilities as NP bf16 pieces, the last one cut off (three hold every bit), a single one rounded.
+template <int NP>
+__device__ __forceinline__ void pieces(float (&x)[8], bf16x8_t (&pf)[NP]) {
+  if constexpr (NP == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pf[0][e] = (__bf16)x[e];
+  } else {
+#pragma unroll
+    for (int pc = 0; pc < NP; ++pc) {
+      pf[pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(x[0], x[1]), high_halves(x[2], x[3]),
+                                                       high_halves(x[4], x[5]), high_halves(x[6], x[7])));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = rest_finite(x[e]);
+    }
+  }
+}
+
+// Products to scores: scale, cap and bias of N values at positions t0 + 32 (j / 8) + 8 g + j % 8. (Without
+// MOD bf16 products stay as they are: the scale goes into the exponent.)
+template <bool MOD, bool F32, int N>
+__device__ __forceinline__ void modify(const Args& a, float* x, const RowLimits& lim, float slope, float inv_cap, int t0, int g) {
+  if constexpr (MOD || F32) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] *= a.scale;
+  }
+  if constexpr (MOD) {
+    if (a.cap > 0.f) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = capped(x[e], a.cap, inv_cap);
+    }
+    if (a.slopes != nullptr) {
+      const float away = (float)(lim.last - t0 - 8 * g);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = fmaf(-slope, away - (float)(32 * (e / 8) + e % 8), x[e]);
+    }
+  }
+}
+
+// KS: 32-wide steps of the head size. MOD: any of cap, slopes, window, mask.
+template <typename TQ, int KS, bool MOD>
 __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
+  constexpr int QT = 1;
   constexpr bool kF32 = sizeof(TQ) == 4;
   constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : 2;  // pieces of queries and probabilities
   constexpr int kHd = KS * 32, DT = KS * 2;
@@ -348,28 +415,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
     const bool there = r < nrows;
     lim[t] = limits<MOD>(a, u, r, nrows);
     slope[t] = MOD && a.slopes != nullptr && there ? a.slopes[h] : 0.f;
-    const TQ* src = static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int c = 4 * s + g;
-      const bool on = there && c < hd8;
-      if constexpr (kF32) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (on) {
-          const float4 x = *reinterpret_cast<const float4*>(src + 8 * c), y = *reinterpret_cast<const float4*>(src + 8 * c + 4);
-          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-        }
-#pragma unroll
-        for (int pc = 0; pc < 3; ++pc) {
-          qf[t][s][pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]),
-                                                                  high_halves(v[4], v[5]), high_halves(v[6], v[7])));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
-        }
-      } else {
-        qf[t][s][0] = __builtin_bit_cast(bf16x8_t, on ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0u, 0u, 0u, 0u));
-      }
-    }
+    load_query<TQ, KS, NQ>(static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd,
+                           there, g, hd8, qf[t]);
   }
   float m[QT], l[QT];
   floatx4_t o[QT][DT];  // columns 16 d + 4 g + e of row fr
@@ -431,21 +478,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[4 * h + e] = kF32 ? hi[e] + low[e] : hi[e];
       }
-      if constexpr (MOD || kF32) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= a.scale;
-      }
-      if constexpr (MOD) {
-        if (a.cap > 0.f) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = capped(x[e], a.cap, inv_cap);
-        }
-        if (a.slopes != nullptr) {
-          const float away = (float)(lim[t].last - t0 - 8 * g);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = fmaf(-slope[t], away - (float)e, x[e]);
-        }
-      }
+      modify<MOD, kF32, 8>(a, x, lim[t], slope[t], inv_cap, t0, g);
       // uniform: some row does not see all of it (a mask may hide row p from its own token)
       if (t0 + kTile > min(c1, MOD ? u.p : u.p + 1) || (MOD && t0 < low_last)) {
 #pragma unroll
@@ -479,13 +512,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
       bf16x8_t pf[NP];
-#pragma unroll
-      for (int pc = 0; pc < NP; ++pc) {
-        pf[pc] = __builtin_bit_cast(bf16x8_t, make_uint4(high_halves(pr[0], pr[1]), high_halves(pr[2], pr[3]),
-                                                         high_halves(pr[4], pr[5]), high_halves(pr[6], pr[7])));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pr[e] = rest_finite(pr[e]);
-      }
+      pieces<NP>(pr, pf);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -593,6 +620,265 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
   }
 }
 
+// Query rows by the 64 QT: each wave keeps 16 QT of them for itself, and the four share tiles of 64 positions
+// in LDS (keys row by row, values column by column, 16-byte chunks swizzled so that the 16 rows of
+// an operand read hit all banks). The tile after the next is on its way to registers while one is
+// worked on, and goes to the other LDS buffer behind it: one barrier a tile.
+constexpr int kTileP = 64;
+constexpr int kRing = 256;  // page entries per half of the ring: 2048 positions
+
+template <typename TQ, int KS, int QT, bool MOD>
+__global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
+  constexpr bool kF32 = sizeof(TQ) == 4;
+  constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : 2;
+  constexpr int DT = KS * 2, kC = KS == 2 ? 8 : 16;  // 16-byte chunks of a key row in LDS
+  constexpr int kKLoads = kTileP * kC / kThreads, kVLoads = KS * 32 * 8 / kThreads;
+  constexpr int kKChunks = kTileP * kC, kVChunks = KS * 32 * 8;
+  __shared__ uint4 s_kv[2][kKChunks + kVChunks];
+  __shared__ uint2 s_page[2 * kRing];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int fr = lane & 15, g = lane >> 4, hd8 = a.hd >> 3, ps = a.pg.page_size;
+  // the longest rows of a prompt first; heads fastest, so that with 8 of them a head stays on one XCD
+  const int kvh = blockIdx.x % a.Hkv, rg = a.rgroups - 1 - blockIdx.x / a.Hkv % a.rgroups;
+  const Unit u = find_unit(a, blockIdx.x / (a.Hkv * a.rgroups));
+  if (u.b < 0) return;
+  const int R = a.G * a.pg.n, r0 = rg * 64 * QT, nrows = u.n * a.G;
+  if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
+  if (u.c1 <= u.c0 && !valid(a, u.p, u.n)) {
+    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, nrows, R);
+    return;
+  }
+  if (r0 >= nrows) return;
+  const int nr = min(64 * QT, nrows - r0);
+  const size_t prow = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R;
+  const int last = u.p + (r0 + nr - 1) / a.G;
+  // positions that some row of the group sees
+  const int c1 = min(u.c1, last + 1);
+  int c0 = u.c0;
+  if (MOD && a.window > 0) c0 = max(c0, (u.p + r0 / a.G + 1 - a.window) & ~(kTile - 1));
+  const int w0 = r0 + 16 * QT * wave;  // this wave's rows
+  bf16x8_t qf[QT][KS][NQ];
+  RowLimits lim[QT];
+  float slope[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = w0 + 16 * t + fr, i = r / a.G, h = kvh * a.G + (r - i * a.G);
+    const bool there = r < nrows;
+    lim[t] = limits<MOD>(a, u, r, nrows);
+    slope[t] = MOD && a.slopes != nullptr && there ? a.slopes[h] : 0.f;
+    load_query<TQ, KS, NQ>(static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd,
+                           there, g, hd8, qf[t]);
+  }
+  float m[QT], l[QT];
+  floatx4_t o[QT][DT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m[t] = -FLT_MAX;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
+  const int wlast = w0 < nrows ? u.p + (min(w0 + 16 * QT, nrows) - 1) / a.G : -1;  // the last row this wave sees
+  const int low_last = MOD && a.window > 0 ? max(0, wlast + 1 - a.window) : 0;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  auto stage = [&](int seg) {  // the pages of positions c0 + 2048 seg ..
+    const int pos = c0 + (seg * kRing + tid) * 8;
+    uint2 w = make_uint2(0u, 0u);
+    if (pos < c1) {
+      const int pg = page_of(a.pg, pos), id = a.pg.table[(size_t)u.b * a.pg.max_pages + pg];
+      if (id >= 0 && id < a.pg.n_pages) w = make_uint2((uint32_t)id, (uint32_t)(pos - pg * ps));
+      else if (pos + 8 > u.lo) s_bad = 1;
+    }
+    s_page[(seg & 1) * kRing + tid] = w;
+  };
+  static_assert(kRing == kThreads, "one entry a thread");
+  uint4 kw[kKLoads], vw[kVLoads];
+  const int kc = tid % kC, kr = tid / kC, vc = tid & 7, vr = tid >> 3;
+  auto load = [&](int t0) {
+    const int e0 = (t0 - c0) >> 3;
+#pragma unroll
+    for (int j = 0; j < kKLoads; ++j) {
+      const int r = kr + j * (kThreads / kC);
+      const uint2 pg = s_page[(e0 + (r >> 3)) & (2 * kRing - 1)];
+      kw[j] = kc < hd8 ? reinterpret_cast<const uint4*>(a.pg.k_pages)[(((size_t)pg.x * a.Hkv + kvh) * ps + pg.y + (r & 7)) * hd8 + kc]
+                       : make_uint4(0u, 0u, 0u, 0u);
+    }
+    const uint2 pg = s_page[(e0 + vc) & (2 * kRing - 1)];
+    const uint16_t* vp = a.pg.v_pages + ((size_t)pg.x * a.Hkv + kvh) * a.hd * ps + pg.y;
+#pragma unroll
+    for (int j = 0; j < kVLoads; ++j) {
+      const int d = vr + j * (kThreads / 8);
+      vw[j] = d < a.hd ? *reinterpret_cast<const uint4*>(vp + (size_t)d * ps) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  auto k_at = [&](int pos, int c) {  // chunk of a key row
+    return kC == 16 ? pos * 16 + (c ^ ((pos & 3) | ((pos >> 1) & 12)))
+                    : pos * 8 + (c ^ (((pos >> 1) & 1) | ((pos >> 2) & 6)));
+  };
+  auto v_at = [&](int d, int c) { return kKChunks + d * 8 + (c ^ ((d >> 1) & 7)); };
+  auto store = [&](uint4* buf, int t0) {
+    if (t0 + kTileP > c1) {  // uniform: nothing behind the last row reaches the sums
+      uint32_t keep[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int pos = t0 + 8 * vc + 2 * e;
+        keep[e] = (pos < c1 ? 0xffffu : 0u) | (pos + 1 < c1 ? 0xffff0000u : 0u);
+      }
+#pragma unroll
+      for (int j = 0; j < kVLoads; ++j)
+        vw[j] = make_uint4(vw[j].x & keep[0], vw[j].y & keep[1], vw[j].z & keep[2], vw[j].w & keep[3]);
+    }
+#pragma unroll
+    for (int j = 0; j < kKLoads; ++j) buf[k_at(kr + j * (kThreads / kC), kc)] = kw[j];
+#pragma unroll
+    for (int j = 0; j < kVLoads; ++j) buf[v_at(vr + j * (kThreads / 8), vc)] = vw[j];
+  };
+  auto compute = [&](const uint4* buf, int t0) {
+    if (t0 > wlast) return;  // uniform over the wave
+    const bf16x8_t* frag = reinterpret_cast<const bf16x8_t*>(buf);
+    float x[QT][2][8];  // positions t0 + 32 nb + 8 g + e
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        floatx4_t hi[QT], low[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) hi[t] = low[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const bf16x8_t kf = frag[k_at(32 * nb + 8 * (fr >> 2) + 4 * h + (fr & 3), 4 * s + g)];
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+#pragma unroll
+            for (int pc = NQ - 1; pc > 0; --pc) low[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][pc], low[t], 0, 0, 0);
+            hi[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][0], hi[t], 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[t][nb][4 * h + e] = kF32 ? hi[t][e] + low[t][e] : hi[t][e];
+      }
+    // some row of the wave does not see all of it (a mask may hide row p from its own token)
+    const bool part = t0 + kTileP > min(c1, MOD && a.mask != nullptr ? u.p : u.p + w0 / a.G + 1);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      modify<MOD, kF32, 16>(a, &x[t][0][0], lim[t], slope[t], inv_cap, t0, g);
+      if (part || (MOD && t0 < low_last)) {  // uniform over the wave
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int pos = t0 + 32 * nb + 8 * g + e;
+            const bool seen = MOD ? lim[t].sees(pos) : pos <= lim[t].last;
+            if (!seen || pos >= c1) x[t][nb][e] = -INFINITY;
+          }
+      }
+      float mx = x[t][0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[t][e >> 3][e & 7]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float c = MOD ? 1.44269504088896341f : to_exp2;
+      if (__ballot(mx > m[t]) != 0) {  // a new maximum: rare behind a row's first tiles
+        const float m_new = fmaxf(m[t], mx);
+        const float alpha = kF32 ? exp_neg(m[t] - m_new) : __builtin_amdgcn_exp2f((m[t] - m_new) * c);
+        m[t] = m_new;
+        l[t] *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[t][nb][e] = kF32 ? exp_neg(x[t][nb][e] - m[t]) : __builtin_amdgcn_exp2f((x[t][nb][e] - m[t]) * c);
+          sum += x[t][nb][e];
+        }
+      l[t] += sum;
+    }
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+      bf16x8_t pf[QT][NP];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) pieces<NP>(x[t][nb], pf[t]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const bf16x8_t vf = frag[v_at(16 * d + fr, 4 * nb + g)];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int pc = NP - 1; pc >= 0; --pc) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][pc], o[t][d], 0, 0, 0);
+      }
+    }
+  };
+  if (c0 < c1) {
+    stage(0);
+    __syncthreads();
+    load(c0);
+    store(s_kv[0], c0);
+    int seg = 0;
+    for (int t0 = c0, i = 0; t0 < c1; t0 += kTileP, ++i) {
+      if (i % (kRing * 8 / kTileP) == 0) stage(++seg);  // read from the last tile of this half on
+      __syncthreads();
+      if (t0 + kTileP < c1) load(t0 + kTileP);
+      compute(s_kv[i & 1], t0);
+      if (t0 + kTileP < c1) store(s_kv[(i + 1) & 1], t0 + kTileP);
+    }
+  }
+  __syncthreads();
+  if (s_bad) {
+    not_a_number<TQ>(a, u, kvh, r0, r0 + nr, R);
+    return;
+  }
+  bool odd = false;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] += __shfl_xor(l[t], 16, kWave);
+    l[t] += __shfl_xor(l[t], 32, kWave);
+    floatx4_t chk = floatx4_t{l[t], 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DT; ++d) chk += o[t][d];
+    odd |= !(fabsf((chk[0] + chk[1]) + (chk[2] + chk[3])) < INFINITY);
+  }
+  if (__ballot(odd) != 0) {
+    Unit w = u;
+    w.c0 = c0;
+    w.c1 = c1;
+    for (int r = w0; r < min(w0 + 16 * QT, nrows); ++r)
+      whole_row<TQ>(a, w, r, kvh, u.count > 1 ? a.po + (prow + r) * a.hd : nullptr, a.pm + prow + r, a.pl + prow + r);
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = w0 + 16 * t + fr;
+    if (r >= nrows) continue;
+    const float unit = kF32 || MOD ? 1.f : a.scale;
+    if (u.count > 1) {
+      if (g == 0) {
+        a.pm[prow + r] = l[t] > 0.f ? m[t] * unit : -INFINITY;
+        a.pl[prow + r] = l[t];
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (16 * d + 4 * g < a.hd)
+          *reinterpret_cast<float4*>(a.po + (prow + r) * a.hd + 16 * d + 4 * g) = make_float4(o[t][d][0], o[t][d][1], o[t][d][2], o[t][d][3]);
+    } else {
+      const int i = r / a.G, h = kvh * a.G + (r - i * a.G);
+      TQ* out = static_cast<TQ*>(a.out) + ((long)(u.first + i) * a.H + h) * a.hd;
+      const float inv = l[t] > 0.f ? 1.f / l[t] : 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        if (16 * d + 4 * g < a.hd)
+          put4(out + 16 * d + 4 * g, make_float4(o[t][d][0] * inv, o[t][d][1] * inv, o[t][d][2] * inv, o[t][d][3] * inv));
+    }
+  }
+}
+
 // The units of a sequence joined in order: one wave per token and head.
 template <typename TQ>
 __global__ __launch_bounds__(kThreads) void attn_paged_merge_kernel(Args a) {
@@ -647,14 +933,17 @@ __global__ __launch_bounds__(kThreads) void attn_paged_merge_kernel(Args a) {
   }
 }
 
-int tiles_of(int rows) { return rows <= 16 ? 1 : 2; }  // query tiles of a workgroup
+// Query rows of a workgroup: up to 32 rows by the sixteen on the kernel without LDS, more by 64, and
+// bf16 ones by 128 where there are that many.
+constexpr int kFewRows = 32;
+int group_rows(int rows, bool bf16) { return rows <= kFewRows ? 16 : !bf16 || rows <= 64 ? 64 : 128; }
 
 }  // namespace
 
-PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd) {
+PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16) {
   PagedAttnLayout L{};
   const int R = H / Hkv * n;
-  L.rgroups = ceil_div(std::max(R, 1), 16 * tiles_of(R));
+  L.rgroups = ceil_div(std::max(R, 1), group_rows(R, bf16));
   const long wgs = (long)Hkv * L.rgroups;
   L.units = (int)std::min<long>((kTargetWgs + wgs - 1) / wgs, kMaxUnits);
   // A unit is at least the average row count over `units`: sequences of more than one unit make fewer
@@ -683,26 +972,31 @@ hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* 
   a.pl = reinterpret_cast<float*>(ws + L.pl);
   a.po = reinterpret_cast<float*>(ws + L.po);
   const bool mod = c.cap > 0.f || c.slopes != nullptr || c.window > 0 || c.mask != nullptr;
-  const int R = a.G * pg.n, qt = tiles_of(R), ks = ceil_div(c.hd, 32);
+  const int R = a.G * pg.n, rows = group_rows(R, c.q_bf16), ks = ceil_div(c.hd, 32);
   // every sequence has a unit, and the cuts add fewer than `units`
   const long grid = (long)c.Hkv * L.rgroups * (pg.B + (L.units > 1 ? L.units : 0));
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   {
     ProfScope prof("attn_paged", stream);
-#define SIRIUS_ROWS(TQ, KS, QT)                                                                     \
-  (mod ? klaunch(attn_rows_kernel<TQ, KS, QT, true>, (int)grid, kThreads, 0, stream, a)                  \
-       : klaunch(attn_rows_kernel<TQ, KS, QT, false>, (int)grid, kThreads, 0, stream, a))
-#define SIRIUS_ROWS_KS(TQ, QT)                                                                      \
-  (ks <= 2 ? SIRIUS_ROWS(TQ, 2, QT) : ks == 3 ? SIRIUS_ROWS(TQ, 3, QT) : SIRIUS_ROWS(TQ, 4, QT))
-    if (c.q_bf16) {
-      if (qt == 1) SIRIUS_ROWS_KS(uint16_t, 1);
-      else SIRIUS_ROWS_KS(uint16_t, 2);
-    } else {
-      if (qt == 1) SIRIUS_ROWS_KS(float, 1);
-      else SIRIUS_ROWS_KS(float, 2);
-    }
-#undef SIRIUS_ROWS_KS
-#undef SIRIUS_ROWS
+    auto launch = [&](auto tq, auto kss, auto mods) {
+      using TQ = decltype(tq);
+      constexpr int KS = decltype(kss)::value;
+      constexpr bool MOD = decltype(mods)::value;
+      if (rows == 16) klaunch(attn_rows_kernel<TQ, KS, MOD>, (int)grid, kThreads, 0, stream, a);
+      else if (rows == 64) klaunch(attn_tiles_kernel<TQ, KS, 1, MOD>, (int)grid, kThreads, 0, stream, a);
+      else if constexpr (sizeof(TQ) == 2) klaunch(attn_tiles_kernel<TQ, KS, 2, MOD>, (int)grid, kThreads, 0, stream, a);
+    };
+    auto by_size = [&](auto tq, auto mods) {
+      if (ks <= 2) launch(tq, std::integral_constant<int, 2>{}, mods);
+      else if (ks == 3) launch(tq, std::integral_constant<int, 3>{}, mods);
+      else launch(tq, std::integral_constant<int, 4>{}, mods);
+    };
+    auto by_mods = [&](auto tq) {
+      if (mod) by_size(tq, std::true_type{});
+      else by_size(tq, std::false_type{});
+    };
+    if (c.q_bf16) by_mods(uint16_t{});
+    else by_mods(float{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -252,7 +252,7 @@ struct PagedAttnLayout {
   int rgroups, units;               // query-row groups per kv head, ranges that the call is cut into
   size_t info, pm, pl, po, total;   // where sequences' partials lie; per unit and row: max, sum, output
 };
-PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd);
+PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16);
 // q [T][H][hd] (token stride ldq), out [T][H][hd] of the same type; cap 0, slopes null, window 0, mask null: none.
 struct PagedAttnCall {
   const void* q;
