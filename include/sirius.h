@@ -557,8 +557,9 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
  * the tokens that see a row on a page outside [0, n_pages) (the sequence's other tokens may);
  * pages in front of every token's window are not looked at.
  * Scores, softmax and the weighted sum are fp32 on the stored bf16 keys and values: fp32 queries and
- * probabilities enter the matrix products in pieces that hold every bit, and with bf16 queries the
- * probabilities hold 16 bits.
+ * probabilities enter the matrix products in pieces that hold every bit. With bf16 queries the
+ * probabilities enter with 16 bits, or where H / n_kv_heads * max_n is above 64 rounded to bf16 (as
+ * are the terms of the sum that they are divided by).
  * Needs sirius_workspace_size(SIRIUS_OP_ATTN_PAGED, ...) for the call's B and max_n.
  * T == 0 and B == 0 are valid no-ops. Errors: SIRIUS_EINVAL as sirius_kv_append for q and the
  * cache, H not a multiple of n_kv_heads, scale < 0 or not finite, softcap < 0 or not finite,

@@ -33,6 +33,8 @@ namespace {
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
 
+typedef unsigned long long u64;
+
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;           // positions per wave step
@@ -68,7 +70,7 @@ __device__ __forceinline__ float rest_finite(float x) {
   return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
 }
 
-// e^x for x <= 0 to about one ulp: exp2 of the rounded x log2(e), times the first order of what the
+// e^x for x <= 4 to about one ulp: exp2 of the rounded x log2(e), times the first order of what the
 // rounding left off. Below -200 (hidden: -inf) 0; a NaN stays one.
 __device__ __forceinline__ float exp_neg(float x) {
   constexpr float kHi = 1.44269502162933349609375f, kLo = 1.9259629911e-8f, kLn2 = 0.693147180559945f;
@@ -429,6 +431,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
   }
   const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
   const int low_last = MOD && a.window > 0 ? max(0, last + 1 - a.window) : 0;  // below it some row sees nothing
+  const float slack = kF32 || MOD ? 4.f : 4.f / a.scale;
   if (tid == 0) s_bad = s_nan = 0;
 
   struct Frag {
@@ -490,27 +493,26 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
       }
       float mx = x[0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      const float m_new = fmaxf(m[t], mx);
-      float alpha, pr[8], sum = 0.f;
-      if constexpr (kF32) {
-        alpha = exp_neg(m[t] - m_new);
+      for (int e = 1; e < 8; ++e) mx = __builtin_elementwise_maximum(mx, x[e]);
+      const float c = MOD ? 1.44269504088896341f : to_exp2;
+      // sums stay on their maximum until some score is e^4 above it (or a NaN)
+      if (__ballot(!(mx <= m[t] + slack)) != 0) {
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 16, kWave));
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, kWave));
+        const float m_new = __builtin_elementwise_maximum(m[t], mx);
+        const float alpha = kF32 ? exp_neg(m[t] - m_new) : __builtin_amdgcn_exp2f((m[t] - m_new) * c);
+        m[t] = m_new;
+        l[t] *= alpha;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pr[e] = exp_neg(x[e] - m_new);
-      } else {
-        const float c = MOD ? 1.44269504088896341f : to_exp2;
-        alpha = __builtin_amdgcn_exp2f((m[t] - m_new) * c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f((x[e] - m_new) * c);
+        for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
       }
+      float pr[8], sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += pr[e];
-      m[t] = m_new;
-      l[t] = fmaf(l[t], alpha, sum);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+      for (int e = 0; e < 8; ++e) {
+        pr[e] = kF32 ? exp_neg(x[e] - m[t]) : __builtin_amdgcn_exp2f((x[e] - m[t]) * c);
+        sum += pr[e];
+      }
+      l[t] += sum;
       bf16x8_t pf[NP];
       pieces<NP>(pr, pf);
 #pragma unroll
@@ -630,14 +632,20 @@ constexpr int kRing = 256;  // page entries per half of the ring: 2048 positions
 template <typename TQ, int KS, int QT, bool MOD>
 __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   constexpr bool kF32 = sizeof(TQ) == 4;
-  constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : 2;
+  constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : QT == 1 ? 2 : 1;
+  // bf16 scores without anything on top: x c - m c in one step, where m starts at a number whose product
+  // is finite (a row with scores below it alone goes the long way)
+  constexpr bool kFused = !kF32 && !MOD;
+  constexpr float kFusedMin = -1e30f;
+  // One rounded piece: the sum is of the rounded probabilities, by a product with ones.
+  constexpr bool kOnes = NP == 1;
   constexpr int DT = KS * 2, kC = KS == 2 ? 8 : 16;  // 16-byte chunks of a key row in LDS
   constexpr int kKLoads = kTileP * kC / kThreads, kVLoads = KS * 32 * 8 / kThreads;
   constexpr int kKChunks = kTileP * kC, kVChunks = KS * 32 * 8;
   __shared__ uint4 s_kv[2][kKChunks + kVChunks];
-  __shared__ uint2 s_page[2 * kRing];
+  __shared__ ulonglong2 s_page[2 * kRing];  // where an 8-position group's keys and values start, in 16-byte units
   __shared__ int s_bad;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 15, g = lane >> 4, hd8 = a.hd >> 3, ps = a.pg.page_size;
   // the longest rows of a prompt first; heads fastest, so that with 8 of them a head stays on one XCD
   const int kvh = blockIdx.x % a.Hkv, rg = a.rgroups - 1 - blockIdx.x / a.Hkv % a.rgroups;
@@ -671,48 +679,54 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
                            there, g, hd8, qf[t]);
   }
   float m[QT], l[QT];
-  floatx4_t o[QT][DT];
+  floatx4_t o[QT][DT], ls[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    m[t] = -FLT_MAX;
+    m[t] = kFused ? kFusedMin : -FLT_MAX;
     l[t] = 0.f;
+    ls[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[t][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   }
   const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
+  const float slack = kF32 || MOD ? 4.f : 4.f / a.scale;
   const int wlast = w0 < nrows ? u.p + (min(w0 + 16 * QT, nrows) - 1) / a.G : -1;  // the last row this wave sees
   const int low_last = MOD && a.window > 0 ? max(0, wlast + 1 - a.window) : 0;
   if (tid == 0) s_bad = 0;
   __syncthreads();
   auto stage = [&](int seg) {  // the pages of positions c0 + 2048 seg ..
     const int pos = c0 + (seg * kRing + tid) * 8;
-    uint2 w = make_uint2(0u, 0u);
+    int id = 0, off = 0;
     if (pos < c1) {
-      const int pg = page_of(a.pg, pos), id = a.pg.table[(size_t)u.b * a.pg.max_pages + pg];
-      if (id >= 0 && id < a.pg.n_pages) w = make_uint2((uint32_t)id, (uint32_t)(pos - pg * ps));
-      else if (pos + 8 > u.lo) s_bad = 1;
+      const int pg = page_of(a.pg, pos);
+      id = a.pg.table[(size_t)u.b * a.pg.max_pages + pg];
+      off = pos - pg * ps;
+      if (id < 0 || id >= a.pg.n_pages) {
+        id = off = 0;
+        if (pos + 8 > u.lo) s_bad = 1;
+      }
     }
-    s_page[(seg & 1) * kRing + tid] = w;
+    const u64 head = (u64)id * a.Hkv + kvh;
+    s_page[(seg & 1) * kRing + tid] = make_ulonglong2((head * ps + off) * hd8, head * a.hd * (ps >> 3) + (off >> 3));
   };
   static_assert(kRing == kThreads, "one entry a thread");
   uint4 kw[kKLoads], vw[kVLoads];
   const int kc = tid % kC, kr = tid / kC, vc = tid & 7, vr = tid >> 3;
+  static_assert(kThreads / kC % 8 == 0, "a thread's key rows are one row of their groups");
+  // Every load is made by every thread: a load under a condition waits for the ones before it. Columns
+  // behind the head's read its last ones and are zeroed on the way into LDS.
+  const uint4* kbase = reinterpret_cast<const uint4*>(a.pg.k_pages) + (kr & 7) * hd8 + min(kc, hd8 - 1);
+  const uint4* vbase[kVLoads];
+#pragma unroll
+  for (int j = 0; j < kVLoads; ++j)
+    vbase[j] = reinterpret_cast<const uint4*>(a.pg.v_pages) + min(vr + j * (kThreads / 8), a.hd - 1) * (ps >> 3);
   auto load = [&](int t0) {
     const int e0 = (t0 - c0) >> 3;
 #pragma unroll
-    for (int j = 0; j < kKLoads; ++j) {
-      const int r = kr + j * (kThreads / kC);
-      const uint2 pg = s_page[(e0 + (r >> 3)) & (2 * kRing - 1)];
-      kw[j] = kc < hd8 ? reinterpret_cast<const uint4*>(a.pg.k_pages)[(((size_t)pg.x * a.Hkv + kvh) * ps + pg.y + (r & 7)) * hd8 + kc]
-                       : make_uint4(0u, 0u, 0u, 0u);
-    }
-    const uint2 pg = s_page[(e0 + vc) & (2 * kRing - 1)];
-    const uint16_t* vp = a.pg.v_pages + ((size_t)pg.x * a.Hkv + kvh) * a.hd * ps + pg.y;
+    for (int j = 0; j < kKLoads; ++j) kw[j] = kbase[s_page[(e0 + (kr >> 3) + j * (kThreads / kC / 8)) & (2 * kRing - 1)].x];
+    const u64 vo = s_page[(e0 + vc) & (2 * kRing - 1)].y;
 #pragma unroll
-    for (int j = 0; j < kVLoads; ++j) {
-      const int d = vr + j * (kThreads / 8);
-      vw[j] = d < a.hd ? *reinterpret_cast<const uint4*>(vp + (size_t)d * ps) : make_uint4(0u, 0u, 0u, 0u);
-    }
+    for (int j = 0; j < kVLoads; ++j) vw[j] = vbase[j][vo];
   };
   auto k_at = [&](int pos, int c) {  // chunk of a key row
     return kC == 16 ? pos * 16 + (c ^ ((pos & 3) | ((pos >> 1) & 12)))
@@ -730,6 +744,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
 #pragma unroll
       for (int j = 0; j < kVLoads; ++j)
         vw[j] = make_uint4(vw[j].x & keep[0], vw[j].y & keep[1], vw[j].z & keep[2], vw[j].w & keep[3]);
+    }
+    if (a.hd < 32 * KS || kC > 4 * KS) {  // uniform
+#pragma unroll
+      for (int j = 0; j < kKLoads; ++j)
+        if (kc >= hd8) kw[j] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int j = 0; j < kVLoads; ++j)
+        if (vr + j * (kThreads / 8) >= a.hd) vw[j] = make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int j = 0; j < kKLoads; ++j) buf[k_at(kr + j * (kThreads / kC), kc)] = kw[j];
@@ -768,6 +790,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
     for (int t = 0; t < QT; ++t) {
       modify<MOD, kF32, 16>(a, &x[t][0][0], lim[t], slope[t], inv_cap, t0, g);
       if (part || (MOD && t0 < low_last)) {  // uniform over the wave
+        asm volatile("");  // a branch, not 48 instructions of every tile
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -779,25 +802,30 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
       }
       float mx = x[t][0][0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[t][e >> 3][e & 7]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      for (int e = 1; e < 16; ++e) mx = __builtin_elementwise_maximum(mx, x[t][e >> 3][e & 7]);
       const float c = MOD ? 1.44269504088896341f : to_exp2;
-      if (__ballot(mx > m[t]) != 0) {  // a new maximum: rare behind a row's first tiles
-        const float m_new = fmaxf(m[t], mx);
+      // Sums stay on their maximum until some score is e^4 above it (or a NaN): rare behind a row's
+      // first tiles, so the lanes of a row seldom have to agree on a new one
+      if (__ballot(!(mx <= m[t] + slack)) != 0) {
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 16, kWave));
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, kWave));
+        const float m_new = __builtin_elementwise_maximum(m[t], mx);
         const float alpha = kF32 ? exp_neg(m[t] - m_new) : __builtin_amdgcn_exp2f((m[t] - m_new) * c);
         m[t] = m_new;
         l[t] *= alpha;
+        ls[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
       }
       float sum = 0.f;
+      const float mc = m[t] * c;
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[t][nb][e] = kF32 ? exp_neg(x[t][nb][e] - m[t]) : __builtin_amdgcn_exp2f((x[t][nb][e] - m[t]) * c);
-          sum += x[t][nb][e];
+          float& y = x[t][nb][e];
+          y = kF32 ? exp_neg(y - m[t]) : __builtin_amdgcn_exp2f(kFused ? fmaf(y, c, -mc) : (y - m[t]) * c);
+          if (!kOnes) sum += y;
         }
       l[t] += sum;
     }
@@ -806,6 +834,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
       bf16x8_t pf[QT][NP];
 #pragma unroll
       for (int t = 0; t < QT; ++t) pieces<NP>(x[t][nb], pf[t]);
+      if constexpr (kOnes) {
+        const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+#pragma unroll
+        for (int t = 0; t < QT; ++t) ls[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t][0], ls[t], 0, 0, 0);
+      }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const bf16x8_t vf = frag[v_at(16 * d + fr, 4 * nb + g)];
@@ -840,6 +873,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   for (int t = 0; t < QT; ++t) {
     l[t] += __shfl_xor(l[t], 16, kWave);
     l[t] += __shfl_xor(l[t], 32, kWave);
+    if (kOnes) l[t] = ls[t][0];
+    if (kFused) odd |= !(l[t] > 0.f) && lim[t].last >= c0;
     floatx4_t chk = floatx4_t{l[t], 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) chk += o[t][d];
