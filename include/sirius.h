@@ -579,8 +579,8 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
  *   ones with w >= m; the best one always.
  * The token is the first one in index order whose running kept mass exceeds u times the kept
  * mass (u is clamped to [0, 1]; at 1 the last kept token of positive mass).
- * Weights are formed in fp64 and added as whole numbers of 2^-(62 - ceil(log2 V)), so a call's
- * result does not depend on the order of its sums.
+ * Weights hold at least 33 bits and are added as whole numbers of 2^-min(50, 62 - ceil(log2 V)) of the best
+ * one's, so a call's result does not depend on the order of its sums.
  *   logits [B, V] fp32, rows ld elements apart (ld >= V; 16-byte aligned base).
  *   u      [B] fp32.
  *   temperature [B] fp32 or NULL (1); 0 is greedy: the argmax, lowest index on ties.
@@ -638,7 +638,7 @@ int sirius_fill_normal_bf16(uint16_t* out, size_t n, uint64_t seed, float mean, 
  * "tree_topw", "tree_select"; "griffin_z", "griffin_rownorm", "griffin_score",
  * "griffin_topk", "condense"; "rmsnorm", "fill_normal"; "attn_partial",
  * "attn_combine", "kv_rollback"; "rope", "kv_append",
- * "attn_paged", "attn_paged_merge"; "sample_row".
+ * "attn_paged", "attn_paged_merge"; "sample_chunk", "sample_finish".
  * sirius_profile_reset drops every record (it waits for pending events).
  * Errors: SIRIUS_EINVAL for NULL arguments, SIRIUS_EHIP if an event fails.
  */

@@ -269,7 +269,7 @@ hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* 
                              hipStream_t stream);
 
 struct SampleLayout {
-  size_t total;
+  size_t stat, list, total;  // what each chunk of a row says of itself; its tokens or bins
 };
 SampleLayout sample_layout(int B, int V);
 // logits [B][V] (row stride ld, 16-byte aligned base); the parameters [B] each, or null.

@@ -10,10 +10,19 @@
 // depend on their order: the histograms below are filled by atomics and every call gives the same
 // token. A row's sums carry an error of about 2^-s sqrt(V) of the best token's weight.
 //
-// sample_row_kernel: one workgroup per row. The cut is found digit by digit (11, 11, 10 bits of the
-// logit's ordered bits): counts and masses per digit, the digit that holds the cut, the next one
-// within it. A last pass adds the kept mass per tile of the row and the tile that holds the draw is
-// looked through token by token.
+// sample_chunk_kernel: one workgroup per chunk of a row, its logits in registers: the chunk's best
+// token, and what the row's filters need,
+//   few (1 < k <= 256)   the tokens that may be among the row's first k: those above a bound that at
+//                        least k of the chunk reach (the k-th of the maxima of 1024 groups);
+//   other filters        the chunk's mass, and counts and masses by bins of an eighth of a temperature,
+//                        down to the lightest token that a cut can fall on;
+//   none                 the chunk's mass.
+// sample_finish_kernel: one workgroup per row. Few: the chunks' tokens above the best bound, sorted in
+// LDS; everything is decided on them. Otherwise the bins give the cut's bin, whose tokens are
+// gathered from the row and sorted; the chunks' kept masses give the chunk of the draw, and its tokens
+// the draw. Rows that none of this fits (lists that overflow, a cut below 32 temperatures, infinite
+// logits) take the long way, row_cut: the cut digit by digit (11, 11, 10 bits of the logit's ordered
+// bits), each by a pass over the row.
 #include <float.h>
 #include <math.h>
 
@@ -29,6 +38,13 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 constexpr int kTiles = 4096;      // tiles of a row at most
 constexpr int kTile = kThreads;   // tokens per tile, a multiple of this where the row has more tiles
+constexpr int kChunkThreads = 256;
+constexpr int kFew = 256;         // the largest k that goes by lists
+constexpr int kList = 512;        // entries of a chunk's list
+constexpr int kSort = 4096;       // tokens that are sorted in LDS at most
+constexpr int kFine = 256;        // bins of an eighth of a temperature; the last one is never counted
+constexpr int kMaxChunks = 2048;  // 2^24 tokens by 8192
+constexpr int kTable = 512;       // powers of two
 
 typedef unsigned long long u64;
 
@@ -45,11 +61,61 @@ struct Args {
   int32_t* token;
   int32_t* kept;
   float* prob;
+  int chunk, chunks;  // tokens per chunk, chunks per row
+  struct ChunkStat* stat;  // [B][chunks]
+  u64* list;               // [B][chunks][kList]: key << 32 | ~index, or kFine masses and kFine / 2 pairs of counts
 };
 
-// Ordered bits: larger logits have larger keys; a NaN counts as -infinity.
+// What a chunk says of itself.
+struct ChunkStat {
+  float best, least;  // least: of its finite logits
+  int best_at, finite;
+  int listed;         // few: tokens on its list (more than kList: it overflowed)
+  uint32_t bound;     // few: at least k tokens reach this key, 0: unknown
+  u64 mass;           // in units of its own best
+};
+
+constexpr int kNone = 0, kByList = 1, kByBins = 2, kWhole = 3;  // kNone: bad parameters, or greedy
+
+// A row's parameters and what they ask for.
+struct Ask {
+  float temp, top_p, min_p, u;
+  int top_k, mode;
+  bool bad, greedy;
+};
+__device__ __forceinline__ Ask ask_of(const Args& a, int b) {
+  Ask q;
+  q.temp = a.temperature != nullptr ? a.temperature[b] : 1.f;
+  q.top_p = a.top_p != nullptr ? a.top_p[b] : 1.f;
+  q.min_p = a.min_p != nullptr ? a.min_p[b] : 0.f;
+  q.top_k = a.top_k != nullptr ? a.top_k[b] : 0;
+  q.u = a.u[b];
+  q.bad = !(q.temp >= 0.f && q.temp < INFINITY && q.top_p == q.top_p && q.min_p == q.min_p && q.u == q.u);
+  q.greedy = q.temp == 0.f || q.top_k == 1 || q.top_p <= 0.f || q.min_p > 1.f;
+  if (q.top_k >= a.V) q.top_k = 0;
+  q.mode = q.bad || q.greedy ? kNone
+           : q.top_k > 0 && q.top_k <= kFew ? kByList
+           : q.top_k > 0 || q.top_p < 1.f || q.min_p > 0.f ? kByBins
+                                                           : kWhole;
+  return q;
+}
+// Bins per unit of logit. The bin of x counts down from the bin of the best: floor(best s) - floor(x s), the same
+// in every kernel; exact while the floors stay below 2^23.
+__device__ __forceinline__ float bin_scale(const Ask& q) { return 8.f / q.temp; }
+__device__ __forceinline__ float bin_of(float x, float s) { return floorf(x * s); }
+// The last bin that a cut can lie in: tokens lighter than (1 - p) / V of the best weigh less than
+// (1 - p) of the row together, and those below min_p of it are out. Some more for the roundings.
+__device__ __forceinline__ int last_bin(const Ask& q, int V) {
+  if (q.top_k > 0) return kFine - 2;
+  float z = -1e30f;
+  if (q.top_p < 1.f) z = logf((1.f - q.top_p) / (float)V);
+  if (q.min_p > 0.f) z = fmaxf(z, logf(q.min_p));
+  return (int)fminf(kFine - 2.f, 8.f * -z + 4.f);
+}
+
+// Ordered bits: larger logits have larger keys, equal ones (0 and -0) the same; a NaN counts as -infinity.
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x == x ? x : -INFINITY);
+  const uint32_t b = __float_as_uint(x == x ? x + 0.f : -INFINITY);
   return b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float logit_of(uint32_t key) {
@@ -146,67 +212,34 @@ struct Cut {
   u64 mass;
 };
 
-template <bool ALIGNED>
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
-  __shared__ u64 s_mass[kTiles];       // histogram or tiles
-  __shared__ uint32_t s_count[kTiles];
-  __shared__ int s_c[kWaves];
-  __shared__ u64 s_m[kWaves];
-  __shared__ float s_x[kWaves];
-  __shared__ int s_i[kWaves];
-  __shared__ int s_bin, s_bc;
-  __shared__ u64 s_bm;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
-  const int b = blockIdx.x, V = a.V;
-  const float* row = a.logits + (long)b * a.ld;
-  const float temp = a.temperature != nullptr ? a.temperature[b] : 1.f;
-  const float top_p = a.top_p != nullptr ? a.top_p[b] : 1.f, min_p = a.min_p != nullptr ? a.min_p[b] : 0.f;
-  const int top_k = a.top_k != nullptr ? a.top_k[b] : 0;
-  const float uu = a.u[b];
-  // ---- the best token: the lowest index of the largest logit
-  float best = -INFINITY;
-  int bi = INT32_MAX;
-  for (int v0 = 4 * tid; v0 < V; v0 += 4 * kThreads) {
-    float x[4];
-    load4<ALIGNED>(row, V, v0, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (x[e] > best) {
-        best = x[e];
-        bi = v0 + e;
-      }
-  }
-  auto better = [](float& v, int& i, float ov, int oi) {
-    if (ov > v || (ov == v && oi < i)) {
-      v = ov;
-      i = oi;
-    }
+struct Shared {
+  union {
+    u64 mass[kTiles];    // the long way: a histogram, or the tiles' masses
+    u64 sorted[kSort];
   };
-  for (int o = 1; o < kWave; o <<= 1) {
-    const float ov = __shfl_xor(best, o, kWave);
-    const int oi = __shfl_xor(bi, o, kWave);
-    better(best, bi, ov, oi);
-  }
-  if (lane == 0) {
-    s_x[wave] = best;
-    s_i[wave] = bi;
-  }
-  __syncthreads();
-  best = s_x[0];
-  bi = s_i[0];
-  for (int w = 1; w < kWaves; ++w) better(best, bi, s_x[w], s_i[w]);
-  const bool ok = temp >= 0.f && temp < INFINITY && top_p == top_p && min_p == min_p && uu == uu && best > -INFINITY;
-  const bool greedy = temp == 0.f || top_k == 1 || top_p <= 0.f || min_p > 1.f;
-  if (!ok || greedy) {  // uniform
-    if (tid == 0) {
-      a.token[b] = ok ? bi : -1;
-      if (a.kept != nullptr) a.kept[b] = ok ? 1 : 0;
-      if (a.prob != nullptr) a.prob[b] = ok ? 1.f : 0.f;
-    }
-    return;
-  }
-  const Weigh wg{(double)best, 1.0 / (double)temp, a.shift};
-  Cut cut{0, INT32_MAX, 0, 0};  // everything
+  union {
+    uint32_t count[kTiles];
+    struct {
+      u64 few_mass[kFew];
+      uint32_t few_at[kFew];
+    };
+  };
+  u64 chunk_mass[kMaxChunks];
+  int scan_c[kWaves];
+  u64 scan_m[kWaves];
+  float x[kWaves];
+  int i[kWaves];
+  int bin, bc;
+  u64 bm;
+  int n;
+};
+
+// The long way, over the whole row.
+template <bool ALIGNED>
+__device__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Shared& sh) {
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, V = a.V;
+  const float* row = a.logits + (long)b * a.ld;
+    Cut cut{0, INT32_MAX, 0, 0};  // everything
   // ---- one cut: the first `want` tokens, or (want < 0) the tokens in front of which less than `share`
   // units lie; of the tokens that `cut` leaves
   auto refine = [&](int want, double share) {
@@ -217,8 +250,8 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
     for (int level = 0; level < 3; ++level) {
       const int bits = level < 2 ? 11 : 10, low = shift - bits;
       for (int i = tid; i < kBins; i += kThreads) {
-        s_mass[i] = 0;
-        s_count[i] = 0;
+        sh.mass[i] = 0;
+        sh.count[i] = 0;
       }
       __syncthreads();
       for (int v0 = 4 * tid; v0 < V; v0 += 4 * kThreads) {
@@ -231,27 +264,27 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
           const double w = wg.weight(x[e]);
           if (w == 0.0) continue;
           const int bin = key >> low & ((1u << bits) - 1);
-          atomicAdd(&s_count[bin], 1u);
-          atomicAdd(&s_mass[bin], wg.units(w));
+          atomicAdd(&sh.count[bin], 1u);
+          atomicAdd(&sh.mass[bin], wg.units(w));
         }
       }
       __syncthreads();
       if (tid == 0 && cut.key != 0 && (level == 0 || cut.key >> shift == prefix)) {  // the ties that the cut before left
         const int bin = cut.key >> low & ((1u << bits) - 1);
-        s_count[bin] += cut.ties;
-        s_mass[bin] += cut.ties * wg.units(wg.weight(logit_of(cut.key)));
+        sh.count[bin] += cut.ties;
+        sh.mass[bin] += cut.ties * wg.units(wg.weight(logit_of(cut.key)));
       }
       __syncthreads();
       const int hi = kBins - 1 - 2 * tid;  // two bins a thread, the largest logits first
-      const int c0 = s_count[hi], c1 = s_count[hi - 1];
-      const u64 m0 = s_mass[hi], m1 = s_mass[hi - 1];
-      const Scan sc = block_scan(c0 + c1, m0 + m1, s_c, s_m);
+      const int c0 = sh.count[hi], c1 = sh.count[hi - 1];
+      const u64 m0 = sh.mass[hi], m1 = sh.mass[hi - 1];
+      const Scan sc = block_scan(c0 + c1, m0 + m1, sh.scan_c, sh.scan_m);
       if (level == 0 && (want >= 0 ? sc.ct <= want : !((double)sc.mt >= share))) {  // uniform: everything stays
         cut.count = sc.ct;
         cut.mass = sc.mt;
         return;
       }
-      if (tid == 0) s_bin = -1;
+      if (tid == 0) sh.bin = -1;
       __syncthreads();
       int bc = above_c + sc.c - c0 - c1;
       u64 bm = above_m + sc.m - m0 - m1;
@@ -262,22 +295,22 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
         // the cut's bin: the first whose end reaches it
         const bool before = want >= 0 ? bc < want : (double)bm < share, after = want >= 0 ? bc + c >= want : (double)(bm + m) >= share;
         if (c > 0 && before && after) {
-          s_bin = hi - k;
-          s_bc = bc;
-          s_bm = bm;
+          sh.bin = hi - k;
+          sh.bc = bc;
+          sh.bm = bm;
         }
         bc += c;
         bm += m;
       }
       __syncthreads();
-      prefix = prefix << bits | (uint32_t)s_bin;
-      above_c = s_bc;
-      above_m = s_bm;
+      prefix = prefix << bits | (uint32_t)sh.bin;
+      above_c = sh.bc;
+      above_m = sh.bm;
       shift = low;
       __syncthreads();
     }
     const u64 each = wg.units(wg.weight(logit_of(prefix)));
-    const int there = (int)s_count[prefix & 1023];
+    const int there = (int)sh.count[prefix & 1023];
     int ties;
     if (want >= 0) ties = want - above_c;
     else ties = each > 0 ? (int)min(ceil((share - (double)above_m) / (double)each), 2147483647.0) : there;
@@ -285,8 +318,8 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
     cut = Cut{prefix, ties, above_c + ties, above_m + ties * each};
     __syncthreads();
   };
-  const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.f;
-  if (by_k) refine(top_k, 0.0);
+  const bool by_k = q.top_k > 0, by_p = q.top_p < 1.f;
+  if (by_k) refine(q.top_k, 0.0);
   if (by_p) {
     if (!by_k) {  // the whole mass first
       u64 m = 0;
@@ -296,14 +329,14 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) m += wg.units(wg.weight(x[e]));
       }
-      cut.mass = block_scan(0, m, s_c, s_m).mt;
+      cut.mass = block_scan(0, m, sh.scan_c, sh.scan_m).mt;
       __syncthreads();
     }
-    refine(-1, (double)top_p * (double)cut.mass);
+    refine(-1, (double)q.top_p * (double)cut.mass);
   }
   // ---- kept mass per tile, ties apart
   const int tile = a.tile, ntiles = (V + tile - 1) / tile;
-  const double floor_w = (double)min_p;
+  const double floor_w = (double)q.min_p;
   const u64 tie_mass = cut.key != 0 ? wg.units(wg.weight(logit_of(cut.key))) : 0;
   const bool ties_stay = cut.key != 0 && wg.weight(logit_of(cut.key)) >= floor_w;
   int kept = 0;
@@ -330,83 +363,614 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(Args a) {
       m += (u64)__shfl_xor((unsigned)(m >> 32), o, kWave) << 32 | __shfl_xor((unsigned)m, o, kWave);
     }
     if (lane == 0) {
-      s_mass[t] = m;
-      s_count[t] = ties_stay ? ties : 0;
+      sh.mass[t] = m;
+      sh.count[t] = ties_stay ? ties : 0;
     }
   }
   for (int i = ntiles + tid; i < kTiles; i += kThreads) {
-    s_mass[i] = 0;
-    s_count[i] = 0;
+    sh.mass[i] = 0;
+    sh.count[i] = 0;
   }
   __syncthreads();
   // four tiles a thread: ties first, then the tiles' masses with the ties that stay
   constexpr int kPer = kTiles / kThreads;
   int tie[kPer], tsum = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) tsum += tie[k] = s_count[kPer * tid + k];
-  const Scan st = block_scan(tsum, 0, s_c, s_m);
+  for (int k = 0; k < kPer; ++k) tsum += tie[k] = sh.count[kPer * tid + k];
+  const Scan st = block_scan(tsum, 0, sh.scan_c, sh.scan_m);
   int before = st.c - tsum;
   u64 mass[kPer], msum = 0;
   int tkept = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int stay = min(max(cut.ties - before, 0), tie[k]);
-    s_count[kPer * tid + k] = min(cut.ties - min(before, cut.ties), INT32_MAX);  // ties that may still stay here
+    sh.count[kPer * tid + k] = min(cut.ties - min(before, cut.ties), INT32_MAX);  // ties that may still stay here
     before += tie[k];
     tkept += stay;
-    mass[k] = s_mass[kPer * tid + k] + stay * tie_mass;
+    mass[k] = sh.mass[kPer * tid + k] + stay * tie_mass;
     msum += mass[k];
   }
-  const Scan sm = block_scan(kept + tkept, msum, s_c, s_m);
-  const double target = (double)fminf(fmaxf(uu, 0.f), 1.f) * (double)sm.mt;
-  if (tid == 0) s_bin = -1;
+  const Scan sm = block_scan(kept + tkept, msum, sh.scan_c, sh.scan_m);
+  const double target = (double)fminf(fmaxf(q.u, 0.f), 1.f) * (double)sm.mt;
+  if (tid == 0) sh.bin = -1;
   __syncthreads();
   // the last tile with mass takes what u = 1 asks for
   u64 run = sm.m - msum;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     if (mass[k] > 0 && (double)run <= target && ((double)(run + mass[k]) > target || run + mass[k] == sm.mt)) {
-      s_bin = kPer * tid + k;
-      s_bm = run;
+      sh.bin = kPer * tid + k;
+      sh.bm = run;
     }
     run += mass[k];
   }
   __syncthreads();
   // ---- the tile, one token a thread
-  const int t = s_bin;
-  u64 ahead = s_bm;
-  int may = (int)s_count[t];
-  if (tid == 0) s_bc = -1;
+  const int t = sh.bin;
+  u64 ahead = sh.bm;
+  int may = (int)sh.count[t];
+  if (tid == 0) sh.bc = -1;
   for (int v0 = t * tile; v0 < min(V, (t + 1) * tile); v0 += kThreads) {
     const int v = v0 + tid;
     const float x = v < V ? row[v] : -INFINITY;
     const uint32_t key = key_of(x);
     const bool tied = v < V && ties_stay && key == cut.key;
-    const Scan tr = block_scan(tied ? 1 : 0, 0, s_c, s_m);
+    const Scan tr = block_scan(tied ? 1 : 0, 0, sh.scan_c, sh.scan_m);
     double w = 0.0;
     if (tied ? tr.c <= may : v < V && key > cut.key) w = wg.weight(x);
     if (w < floor_w) w = 0.0;
     const u64 m = wg.units(w);
-    const Scan ts = block_scan(0, m, s_c, s_m);
+    const Scan ts = block_scan(0, m, sh.scan_c, sh.scan_m);
     const u64 end = ahead + ts.m;
     if (m > 0 && (double)(end - m) <= target && ((double)end > target || end == sm.mt)) {
-      s_bc = v;
+      sh.bc = v;
       a.token[b] = v;
       if (a.prob != nullptr) a.prob[b] = (float)((double)m / (double)sm.mt);
     }
     __syncthreads();
-    if (s_bc >= 0) break;
+    if (sh.bc >= 0) break;
     ahead += ts.mt;
     may -= min(may, tr.ct);
   }
   if (tid == 0 && a.kept != nullptr) a.kept[b] = sm.ct;
 }
 
+
+// 2^(j / 512) for the powers below.
+__device__ __forceinline__ void fill_table(double* table) {
+  for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = 2.0 * exp_nonpos((i - kTable) * (0.69314718055994530942 / kTable));
+}
+// Units of 2^-shift of exp((x - best) / T), y = (x - best) 512 log2(e) / T: a power of two from the table
+// times 1 + g, g = 2^(r / 512) - 1 in fp32 with |r| <= 1/2, so the weight is within 1e-10 of its own value.
+// Whole units come out of the sum with 2^52.
+__device__ __forceinline__ u64 fast_units(double y, int shift, const double* table) {
+  y = fmax(y, -512000.0);
+  const double k = rint(y);
+  const float r = (float)(y - k);
+  const int n = (int)k;
+  constexpr float kL = 0.69314718f / kTable;  // ln 2 / 512
+  const float g = r * fmaf(r, fmaf(r, kL * kL * kL / 6.f, kL * kL / 2.f), kL);
+  const double t = table[n & (kTable - 1)];
+  const double w = ldexp(fma(t, (double)g, t), (n >> 9) + shift);
+  return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;
+}
+
+template <bool ALIGNED, int PER>
+__global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
+  constexpr int kW = kChunkThreads / kWave, kSub = 4;  // groups whose maxima bound the k-th token: 4 a thread
+  __shared__ float s_x[kW], s_y[kW];
+  __shared__ int s_i[kW], s_f[kW], s_n;
+  __shared__ u64 s_m[kW];
+  __shared__ uint32_t s_bound;
+  __shared__ union {
+    uint32_t sub[kSub * kChunkThreads];
+    struct {
+      double table[kTable];
+      u64 mass[kFine];
+      uint32_t count[kFine];
+    };
+  } sh;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int c = blockIdx.x % a.chunks, b = blockIdx.x / a.chunks;
+  const Ask q = ask_of(a, b);
+  if (q.bad) return;
+  const float* row = a.logits + (long)b * a.ld;
+  const int v0 = c * a.chunk;
+  float x[PER][4];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) load4<ALIGNED>(row, a.V, v0 + 4 * (tid + j * kChunkThreads), x[j]);
+  float best = -INFINITY, least = INFINITY;
+  int at = INT32_MAX, finite = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float& y = x[j][e];
+      if (!(y > -INFINITY)) y = -INFINITY;  // NaN too
+      if (y > best) {
+        best = y;
+        at = v0 + 4 * (tid + j * kChunkThreads) + e;
+      }
+      if (y > -INFINITY) {
+        ++finite;
+        least = fminf(least, y);
+      }
+    }
+  for (int o = 1; o < kWave; o <<= 1) {
+    const float ov = __shfl_xor(best, o, kWave);
+    const int oi = __shfl_xor(at, o, kWave);
+    if (ov > best || (ov == best && oi < at)) {
+      best = ov;
+      at = oi;
+    }
+    least = fminf(least, __shfl_xor(least, o, kWave));
+    finite += __shfl_xor(finite, o, kWave);
+  }
+  if (lane == 0) {
+    s_x[wave] = best;
+    s_y[wave] = least;
+    s_i[wave] = at;
+    s_f[wave] = finite;
+  }
+  if (tid == 0) s_n = 0;
+  if (q.mode == kByBins || q.mode == kWhole) fill_table(sh.table);
+  if (q.mode == kByBins) {
+    sh.mass[tid] = 0;
+    sh.count[tid] = 0;
+  }
+  if (q.mode == kByList) {
+#pragma unroll
+    for (int k = 0; k < kSub; ++k) {
+      float m = -INFINITY;  // of PER float4s over kSub groups
+#pragma unroll
+      for (int e = k * PER; e < (k + 1) * PER; ++e) m = fmaxf(m, x[e / 4][e % 4]);
+      sh.sub[k * kChunkThreads + tid] = key_of(m);
+    }
+  }
+  __syncthreads();
+  best = s_x[0];
+  at = s_i[0];
+  least = s_y[0];
+  finite = s_f[0];
+  for (int w = 1; w < kW; ++w) {
+    if (s_x[w] > best || (s_x[w] == best && s_i[w] < at)) {
+      best = s_x[w];
+      at = s_i[w];
+    }
+    least = fminf(least, s_y[w]);
+    finite += s_f[w];
+  }
+  ChunkStat st{best, least, at, finite, 0, 0, 0};
+  u64* list = a.list + ((size_t)b * a.chunks + c) * kList;
+  if (q.mode == kByList) {
+    if (wave == 0) {  // the largest key of 16 bits that k of the groups' maxima reach
+      uint32_t sub[kSub * kW];
+#pragma unroll
+      for (int k = 0; k < kSub * kW; ++k) sub[k] = sh.sub[k * kWave + lane];
+      uint32_t bound = 0;
+      for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < kSub * kW; ++k) n += __popcll(__ballot(sub[k] >= (bound | bit)));
+        if (n >= q.top_k) bound |= bit;
+      }
+      if (lane == 0) s_bound = bound;
+    }
+    __syncthreads();
+    const uint32_t bound = s_bound;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t key = key_of(x[j][e]);
+        if (key >= bound && x[j][e] > -INFINITY) {
+          const int n = atomicAdd(&s_n, 1);
+          if (n < kList) list[n] = (u64)key << 32 | ~(uint32_t)(v0 + 4 * (tid + j * kChunkThreads) + e);
+        }
+      }
+    __syncthreads();
+    st.listed = s_n;
+    st.bound = bound > key_of(-INFINITY) ? bound : 0;
+  } else if (q.mode != kNone && best > -INFINITY) {
+    const double to = kTable * 1.44269504088896340736 / (double)q.temp, off = -(double)best * to;
+    const float s = bin_scale(q), top = bin_of(best, s);
+    const float last = q.mode == kByBins ? (float)last_bin(q, a.V) : -1.f;
+    u64 m = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const u64 w = fast_units(fma((double)x[j][e], to, off), a.shift, sh.table);
+        m += w;
+        const float bin = top - bin_of(x[j][e], s);
+        if (bin <= last) {  // none where bins are not wanted
+          atomicAdd(&sh.mass[(int)bin], w);
+          atomicAdd(&sh.count[(int)bin], 1u);
+        }
+      }
+    for (int o = 1; o < kWave; o <<= 1) m += (u64)__shfl_xor((unsigned)(m >> 32), o, kWave) << 32 | __shfl_xor((unsigned)m, o, kWave);
+    if (lane == 0) s_m[wave] = m;
+    __syncthreads();
+    for (int w = 0; w < kW; ++w) st.mass += s_m[w];
+    if (q.mode == kByBins) {
+      list[tid] = sh.mass[tid];
+      reinterpret_cast<uint32_t*>(list + kFine)[tid] = sh.count[tid];
+    }
+  }
+  if (tid == 0) a.stat[(size_t)b * a.chunks + c] = st;
+}
+
+// Sorts n2 (a power of two) values, the largest first.
+__device__ __forceinline__ void sort_down(u64* v, int n2) {
+  for (int size = 2; size <= n2; size <<= 1)
+    for (int step = size >> 1; step > 0; step >>= 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < n2 >> 1; i += kThreads) {
+        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+        const u64 p = v[lo], r = v[hi];
+        if ((p < r) == ((lo & size) == 0)) {
+          v[lo] = r;
+          v[hi] = p;
+        }
+      }
+    }
+  __syncthreads();
+}
+__device__ __forceinline__ int pad_and_sort(u64* v, int n) {
+  int n2 = 2;
+  while (n2 < n) n2 <<= 1;
+  for (int i = n + threadIdx.x; i < n2; i += kThreads) v[i] = 0;
+  sort_down(v, n2);
+  return n2;
+}
+
+template <bool ALIGNED>
+__global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int b = blockIdx.x, V = a.V;
+  const float* row = a.logits + (long)b * a.ld;
+  const Ask q = ask_of(a, b);
+  const ChunkStat* stat = a.stat + (size_t)b * a.chunks;
+  auto answer = [&](int token, int kept, float prob) {
+    a.token[b] = token;
+    if (a.kept != nullptr) a.kept[b] = kept;
+    if (a.prob != nullptr) a.prob[b] = prob;
+  };
+  if (q.bad) {
+    if (tid == 0) answer(-1, 0, 0.f);
+    return;
+  }
+  // ---- the row's best, its least finite logit and their number; lists that overflowed; the best bound
+  float best = -INFINITY, least = INFINITY;
+  int at = INT32_MAX, finite = 0;
+  uint32_t bound = 0;
+  for (int c = tid; c < a.chunks; c += kThreads) {
+    const ChunkStat st = stat[c];
+    if (st.best > best || (st.best == best && st.best_at < at)) {
+      best = st.best;
+      at = st.best_at;
+    }
+    least = fminf(least, st.least);
+    finite += st.finite;
+    if (q.mode == kByList) bound = max(bound, st.listed > kList ? 0xffffffffu : st.bound);
+  }
+  if (a.chunks > 1) {  // uniform
+    for (int o = 1; o < kWave; o <<= 1) {
+      const float ov = __shfl_xor(best, o, kWave);
+      const int oi = __shfl_xor(at, o, kWave);
+      if (ov > best || (ov == best && oi < at)) {
+        best = ov;
+        at = oi;
+      }
+      least = fminf(least, __shfl_xor(least, o, kWave));
+      finite += __shfl_xor(finite, o, kWave);
+      bound = max(bound, (uint32_t)__shfl_xor((int)bound, o, kWave));
+    }
+  }
+  if (lane == 0) {
+    sh.x[wave] = best;
+    sh.i[wave] = at;
+    sh.scan_c[wave] = finite;
+    sh.scan_m[wave] = (u64)__float_as_uint(least) << 32 | bound;
+  }
+  if (tid == 0) {
+    sh.n = 0;
+    sh.bin = sh.bc = -1;
+  }
+  __syncthreads();
+  const int nw = a.chunks > kThreads - kWave ? kWaves : (a.chunks + kWave - 1) / kWave;  // waves that saw chunks
+  best = sh.x[0];
+  at = sh.i[0];
+  finite = sh.scan_c[0];
+  least = __uint_as_float((uint32_t)(sh.scan_m[0] >> 32));
+  bound = (uint32_t)sh.scan_m[0];
+  for (int w = 1; w < nw; ++w) {
+    if (sh.x[w] > best || (sh.x[w] == best && sh.i[w] < at)) {
+      best = sh.x[w];
+      at = sh.i[w];
+    }
+    finite += sh.scan_c[w];
+    least = fminf(least, __uint_as_float((uint32_t)(sh.scan_m[w] >> 32)));
+    bound = max(bound, (uint32_t)sh.scan_m[w]);
+  }
+  if (best == -INFINITY || q.greedy) {
+    if (tid == 0) {
+      if (best == -INFINITY) answer(-1, 0, 0.f);
+      else answer(at, 1, 1.f);
+    }
+    return;
+  }
+  const Weigh wg{(double)best, 1.0 / (double)q.temp, a.shift};
+  const double share_u = (double)fminf(fmaxf(q.u, 0.f), 1.f);
+  const float s = bin_scale(q), top = bin_of(best, s);
+  // infinite logits; lists that overflowed
+  bool longway = best == INFINITY || bound == 0xffffffffu;
+  if (q.mode == kByList && !longway) {
+    for (int c = wave; c < a.chunks; c += kWaves) {
+      const int n = stat[c].listed;
+      const u64* list = a.list + ((size_t)b * a.chunks + c) * kList;
+      for (int i = lane; i < n; i += kWave) {
+        const u64 e = list[i];
+        if ((uint32_t)(e >> 32) >= bound) {
+          const int to = atomicAdd(&sh.n, 1);
+          if (to < kSort) sh.sorted[to] = e;
+        }
+      }
+    }
+    __syncthreads();
+    const int n = sh.n;
+    longway = n > kSort;
+    if (!longway) {
+      pad_and_sort(sh.sorted, n);
+      // the first k, their masses in order, and how many of them stay
+      double w = 0.0;
+      const u64 mine = tid < min(n, q.top_k) ? sh.sorted[tid] : 0;
+      if (mine != 0) w = wg.weight(logit_of((uint32_t)(mine >> 32)));
+      const u64 m = wg.units(w);
+      const Scan all = block_scan(0, m, sh.scan_c, sh.scan_m);
+      const bool stays = w > 0.0 && (tid == 0 || ((q.top_p >= 1.f || (double)(all.m - m) < (double)q.top_p * (double)all.mt) && w >= (double)q.min_p));
+      const Scan kept = block_scan(stays ? 1 : 0, stays ? m : 0, sh.scan_c, sh.scan_m);
+      if (stays) {
+        sh.few_mass[tid] = m;
+        sh.few_at[tid] = ~(uint32_t)mine;
+      }
+      __syncthreads();
+      if (stays && m > 0) {
+        const uint32_t here = sh.few_at[tid];
+        u64 run = 0;  // mass up to this index
+        for (int i = 0; i < kept.ct; ++i) run += sh.few_at[i] <= here ? sh.few_mass[i] : 0;
+        const double target = share_u * (double)kept.mt;
+        if ((double)(run - m) <= target && ((double)run > target || run == kept.mt))
+          answer((int)here, kept.ct, (float)((double)m / (double)kept.mt));
+      }
+      return;
+    }
+  }
+  // Beside the best a token may weigh nothing although its chunk counted it, and bins have to be exact.
+  if (((double)best - (double)least) * wg.inv_t > 690.0 || !(fabsf(top) < 8388608.f) || !(fabsf(bin_of(least, s)) < 8388608.f)) longway = true;
+  // a mass in units of a chunk's best, in the row's
+  auto scaled = [&](u64 m, float from) { return (u64)rint((double)m * exp_nonpos(((double)from - (double)best) * wg.inv_t)); };
+  auto bins_of = [&](int c) { return a.list + ((size_t)b * a.chunks + c) * kList; };
+  u64 cutoff = 0;        // tokens whose (key, ~index) reaches this stay
+  int kept = finite;
+  int lo = 0, hi = -1;   // the bins whose tokens are in sh.sorted; the bins in front of them stay whole
+  if (q.mode == kByBins && !longway) {
+    const int last = last_bin(q, V);
+    u64 fm = 0, total = 0;
+    int fc = 0;
+    for (int c = tid; c < a.chunks; c += kThreads)
+      if (stat[c].best > -INFINITY) total += scaled(stat[c].mass, stat[c].best);
+    total = block_scan(0, total, sh.scan_c, sh.scan_m).mt;
+    if (tid <= last)
+      for (int c = 0; c < a.chunks; ++c) {
+        const float from = stat[c].best, j = (float)tid - (top - bin_of(from, s));
+        if (!(from > -INFINITY) || !(j >= 0.f)) continue;
+        const u64 m = bins_of(c)[(int)j];
+        if (m != 0) fm += scaled(m, from);
+        fc += (int)reinterpret_cast<const uint32_t*>(bins_of(c) + kFine)[(int)j];
+      }
+    const Scan sc = block_scan(fc, fm, sh.scan_c, sh.scan_m);
+    int above_c = 0;  // tokens and mass in front of bin lo
+    u64 above = 0;
+    // The first bin whose end reaches `want` tokens (want > 0) or `share` units; -1: none.
+    auto find = [&](int want, double share) {
+      __syncthreads();
+      if (tid == 0) sh.bin = -1;
+      __syncthreads();
+      const bool hit = want > 0 ? sc.c - fc < want && sc.c >= want : (double)(sc.m - fm) < share && (double)sc.m >= share;
+      if (tid <= last && fc > 0 && hit) sh.bin = tid;
+      __syncthreads();
+      return sh.bin;
+    };
+    // Bins b0 .. b1 into sh.sorted. false: too many tokens.
+    auto gather = [&](int b0, int b1) {
+      if (b0 == lo && b1 == hi) return true;
+      lo = b0;
+      hi = b1;
+      __syncthreads();
+      if (tid == 0) sh.n = 0;
+      if (tid == b0) {
+        sh.bc = sc.c - fc;
+        sh.bm = sc.m - fm;
+      }
+      __syncthreads();
+      above_c = sh.bc;
+      above = sh.bm;
+      for (int c = wave; c < a.chunks; c += kWaves) {
+        const float from = stat[c].best;
+        if (!(from > -INFINITY) || top - bin_of(from, s) > (float)b1) continue;
+        const int end = min(V, (c + 1) * a.chunk);
+        for (int v0 = c * a.chunk + 4 * lane; v0 < end; v0 += 16 * kWave) {
+          float x[4][4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) load4<ALIGNED>(row, v0 + 4 * k * kWave < end ? V : 0, v0 + 4 * k * kWave, x[k]);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float y = x[k >> 2][k & 3], bin = top - bin_of(y, s);
+            if (bin >= (float)b0 && bin <= (float)b1) {  // no NaN, no infinity
+              const int to = atomicAdd(&sh.n, 1);
+              if (to < kSort) sh.sorted[to] = (u64)key_of(y) << 32 | ~(uint32_t)(v0 + (k >> 2) * 4 * kWave + (k & 3));
+            }
+          }
+        }
+      }
+      __syncthreads();
+      if (sh.n > kSort) return false;
+      pad_and_sort(sh.sorted, sh.n);
+      return true;
+    };
+    // How many of the first `most` tokens of sh.sorted stay, by weight (floor_w > 0) or by the mass in front.
+    auto within = [&](double share, double floor_w, int most) {
+      int n = 0;
+      u64 run = above;
+      for (int i0 = 0; i0 < most; i0 += kThreads) {
+        const int i = i0 + tid;
+        const double w = i < most ? wg.weight(logit_of((uint32_t)(sh.sorted[i] >> 32))) : 0.0;
+        const u64 m = wg.units(w);
+        const Scan t = block_scan(0, m, sh.scan_c, sh.scan_m);
+        const bool stays = i < most && (floor_w > 0.0 ? w >= floor_w : (double)(run + t.m - m) < share);
+        n += block_scan(stays ? 1 : 0, 0, sh.scan_c, sh.scan_m).ct;
+        run += t.mt;
+      }
+      return n;
+    };
+    if (q.top_k > 0 && finite > q.top_k) {
+      const int bin = find(q.top_k, 0.0);
+      if (bin < 0 || !gather(bin, bin)) {
+        longway = true;
+      } else {
+        kept = q.top_k;
+        cutoff = sh.sorted[kept - above_c - 1];
+        u64 m = 0;
+        for (int i = tid; i < kept - above_c; i += kThreads) m += wg.units(wg.weight(logit_of((uint32_t)(sh.sorted[i] >> 32))));
+        total = above + block_scan(0, m, sh.scan_c, sh.scan_m).mt;
+      }
+    }
+    // the lightest logit that min_p leaves lies in bin `edge` or, for its rounding, beside it
+    const float xm = q.min_p > 0.f ? (float)((double)best + (double)q.temp * log((double)q.min_p)) : -INFINITY;
+    const float edge = fmaxf(top - bin_of(xm, s), 0.f);
+    const bool by_m = edge < (float)last;  // else behind the bins: it cuts nothing that another cut leaves
+    bool cut = q.top_k > 0;
+    if (q.top_p < 1.f && !longway) {
+      const double share = (double)q.top_p * (double)total;
+      const int bin = find(0, share);
+      if (bin < 0) {
+        longway = !by_m;  // behind the bins
+      } else if (!gather(bin, bin)) {
+        longway = true;
+      } else {
+        cut = true;
+        const int n = within(share, 0.0, min(sh.n, kept - above_c));
+        if (n > 0 && above_c + n < kept) {
+          kept = above_c + n;
+          cutoff = sh.sorted[n - 1];
+        }
+      }
+    }
+    if (q.min_p > 0.f && !by_m && !cut) longway = true;
+    if (by_m && !longway) {
+      if (!gather(max((int)edge - 1, 0), (int)edge + 1)) {
+        longway = true;
+      } else {
+        const int n = within(0.0, (double)q.min_p, sh.n);
+        if (above_c + n < kept) {
+          kept = above_c + n;
+          cutoff = n > 0 ? sh.sorted[n - 1] : sh.n > 0 ? sh.sorted[0] + 1 : (u64)key_of(xm) << 32;
+        }
+      }
+    }
+    if (!longway && cutoff != 0) {  // the cut's bin among the gathered ones
+      const int bin = (int)(top - bin_of(logit_of((uint32_t)(cutoff >> 32)), s));
+      if ((bin < lo || bin > hi) && (bin < 0 || bin > last || !gather(bin, bin))) longway = true;
+    }
+  }
+  if (longway || q.mode == kByList) {
+    __syncthreads();
+    row_cut<ALIGNED>(a, q, wg, b, sh);
+    return;
+  }
+  // ---- the chunks' kept masses, the chunk of the draw
+  for (int c = wave; c < a.chunks; c += kWaves) {
+    const float from = stat[c].best;
+    u64 m = 0;
+    if (from > -INFINITY) {
+      if (cutoff == 0) {
+        m = lane == 0 ? scaled(stat[c].mass, from) : 0;
+      } else {
+        const int off = (int)(top - bin_of(from, s));  // its bins count from here
+        for (int bin = off + lane; bin < lo; bin += kWave) {
+          const u64 k = bins_of(c)[bin - off];
+          if (k != 0) m += scaled(k, from);
+        }
+      }
+    }
+    for (int o = 1; o < kWave; o <<= 1) m += (u64)__shfl_xor((unsigned)(m >> 32), o, kWave) << 32 | __shfl_xor((unsigned)m, o, kWave);
+    if (lane == 0) sh.chunk_mass[c] = m;
+  }
+  __syncthreads();
+  if (cutoff != 0)
+    for (int i = tid; i < sh.n; i += kThreads) {
+      const u64 e = sh.sorted[i];
+      if (e >= cutoff) atomicAdd(&sh.chunk_mass[~(uint32_t)e / (uint32_t)a.chunk], wg.units(wg.weight(logit_of((uint32_t)(e >> 32)))));
+    }
+  __syncthreads();
+  constexpr int kPer = kMaxChunks / kThreads;
+  u64 cm[kPer], sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) sum += cm[k] = kPer * tid + k < a.chunks ? sh.chunk_mass[kPer * tid + k] : 0;
+  const Scan cs = block_scan(0, sum, sh.scan_c, sh.scan_m);
+  const double target = share_u * (double)cs.mt;
+  u64 run = cs.m - sum;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (cm[k] > 0 && (double)run <= target && ((double)(run + cm[k]) > target || run + cm[k] == cs.mt)) {
+      sh.bin = kPer * tid + k;
+      sh.bm = run;
+    }
+    run += cm[k];
+  }
+  __syncthreads();
+  // ---- its tokens, the same number to each thread
+  const int c = sh.bin, each = a.chunk / kThreads, first = c * a.chunk + tid * each;
+  const double rest = target - (double)sh.bm;
+  u64 m = 0;
+  for (int e = 0; e < each; ++e) {
+    const int v = first + e;
+    const float x = v < V ? row[v] : -INFINITY;
+    if (x > -INFINITY && ((u64)key_of(x) << 32 | ~(uint32_t)v) >= cutoff) m += wg.units(wg.weight(x));
+  }
+  const Scan ts = block_scan(0, m, sh.scan_c, sh.scan_m);
+  // (the chunk's own sum may be some units off: then its last token of positive mass)
+  if (m > 0 && (double)(ts.m - m) <= rest && ((double)ts.m > rest || ts.m == ts.mt)) {
+    u64 before = ts.m - m;
+    for (int e = 0; e < each; ++e) {
+      const int v = first + e;
+      const float x = v < V ? row[v] : -INFINITY;
+      if (!(x > -INFINITY) || ((u64)key_of(x) << 32 | ~(uint32_t)v) < cutoff) continue;
+      const u64 w = wg.units(wg.weight(x));
+      before += w;
+      if (w > 0 && ((double)before > rest || before == ts.mt)) {
+        answer(v, kept, (float)((double)w / (double)cs.mt));
+        break;
+      }
+    }
+  }
+}
+
 }  // namespace
+
+// Tokens per chunk: 8192, or 2048 where a call has fewer chunks than CUs of them (one row of 128256
+// tokens makes 63 workgroups of 2048, not 16).
+static int chunk_of(int B, int V) { return (long)B * ceil_div(V, 8192) < 256 && ceil_div(V, 2048) <= kMaxChunks ? 2048 : 8192; }
 
 SampleLayout sample_layout(int B, int V) {
   SampleLayout L{};
-  L.total = 256;
+  const size_t chunks = (size_t)B * ceil_div(V, chunk_of(B, V));
+  Carve c;
+  L.stat = c.take(chunks * sizeof(ChunkStat));
+  L.list = c.take(chunks * kList * sizeof(u64));
+  L.total = c.off;
   return L;
 }
 
@@ -417,12 +981,29 @@ hipError_t launch_sample(const SampleCall& c, char* ws, const SampleLayout& L, h
   a.token = c.token; a.kept = c.kept; a.prob = c.prob;
   int bits = 0;
   while ((1 << bits) < c.V) ++bits;
-  a.shift = 62 - bits;
+  a.shift = std::min(62 - bits, 50);
   a.tile = kTile * ceil_div(ceil_div(c.V, kTile), kTiles);
+  a.chunk = chunk_of(c.B, c.V);
+  a.chunks = ceil_div(c.V, a.chunk);
+  a.stat = reinterpret_cast<ChunkStat*>(ws + L.stat);
+  a.list = reinterpret_cast<u64*>(ws + L.list);
   const bool aligned = c.ld % 4 == 0 || c.B == 1;
-  ProfScope prof("sample_row", stream);
-  if (aligned) klaunch(sample_row_kernel<true>, c.B, kThreads, 0, stream, a);
-  else klaunch(sample_row_kernel<false>, c.B, kThreads, 0, stream, a);
+  {
+    ProfScope prof("sample_chunk", stream);
+    const int grid = c.B * a.chunks;
+    if (a.chunk == 2048) {
+      if (aligned) klaunch(sample_chunk_kernel<true, 2>, grid, kChunkThreads, 0, stream, a);
+      else klaunch(sample_chunk_kernel<false, 2>, grid, kChunkThreads, 0, stream, a);
+    } else {
+      if (aligned) klaunch(sample_chunk_kernel<true, 8>, grid, kChunkThreads, 0, stream, a);
+      else klaunch(sample_chunk_kernel<false, 8>, grid, kChunkThreads, 0, stream, a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  ProfScope prof("sample_finish", stream);
+  if (aligned) klaunch(sample_finish_kernel<true>, c.B, kThreads, 0, stream, a);
+  else klaunch(sample_finish_kernel<false>, c.B, kThreads, 0, stream, a);
   return hipGetLastError();
 }
 

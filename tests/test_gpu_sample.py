@@ -85,6 +85,35 @@ def test_mixed_batch_and_all_of_u(sr):
     _check(sr, _logits(rng, b, v, ties=True), rng.random(b), t, k, p, m)
 
 
+def test_cuts_far_down_and_crowded(sr):
+    """Cuts below what the bins hold, lists and bins with more tokens than their room, both cuts at once."""
+    rng = np.random.default_rng(21)
+    v = 40000
+    x = _logits(rng, 12, v, std=3.0)
+    x[1] = np.round(x[1])                      # a dozen values: thousands of ties at every cut
+    x[2] = rng.choice([0.0, 1e-3], v)
+    x[3, :20000] -= 200.0                      # half of the row weighs next to nothing
+    x[4, 1:] -= 1000.0                         # more than 700 below: not counted
+    x[5] = np.sort(x[5])
+    x[6] = np.sort(x[6])[::-1]
+    x[7, 5000:] = -np.inf
+    x[8] *= 30.0
+    u = rng.random(12).astype(np.float32)
+    f = lambda a: np.full(12, a, np.float32)
+    for t, k, p, m in ((1.0, 0, 1.0, 1e-15), (1.0, 0, 0.9999999, 0.0), (1.0, 0, 0.9999999, 1e-3), (1.0, 0, 0.3, 1e-20), (1.0, 200, 1.0, 0.0),
+                       (1.0, 256, 0.99, 1e-9), (1.0, 257, 1.0, 0.0), (1.0, 39999, 1.0, 0.0), (1.0, 30000, 0.999, 0.0), (0.01, 300, 0.9, 0.1),
+                       (1.0, 5000, 0.2, 0.3), (1.0, 0, 1.0, 0.0), (0.02, 0, 1.0, 0.0), (1e-6, 0, 0.9, 0.0), (1e-6, 3, 0.9, 0.0), (1e9, 0, 0.5, 0.0)):
+        _check(sr, x, u, f(t), np.full(12, k), f(p), f(m))
+
+
+def test_long_rows_of_many_chunks(sr):
+    rng = np.random.default_rng(22)
+    x = _logits(rng, 2, (1 << 21) + 77)
+    for t, k, p, m in ((1.0, 100, 0.9, 0.0), (1.0, 0, 0.6, 0.0), (1.0, 0, 1.0, 0.02), (1.0, 0, 1.0, 0.0), (1.0, 3000, 0.9, 0.001)):
+        f = lambda a: np.full(2, a, np.float32)
+        _check(sr, x, rng.random(2).astype(np.float32), f(t), np.full(2, k), f(p), f(m))
+
+
 def test_equal_logits(sr):
     """Every border is a tie: the lowest indices stay."""
     x = np.zeros((6, 1000), np.float32)
