@@ -33,11 +33,11 @@
 namespace sirius {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 constexpr int kTiles = 4096;      // tiles of a row at most
-constexpr int kTile = kThreads;   // tokens per tile, a multiple of this where the row has more tiles
+constexpr int kTile = 1024;       // tokens per tile, a multiple of this where the row has more tiles
 constexpr int kChunkThreads = 256;
 constexpr int kFew = 256;         // the largest k that goes by lists
 constexpr int kList = 512;        // entries of a chunk's list
@@ -45,6 +45,7 @@ constexpr int kSort = 4096;       // tokens that are sorted in LDS at most
 constexpr int kFine = 256;        // bins of an eighth of a temperature; the last one is never counted
 constexpr int kMaxChunks = 2048;  // 2^24 tokens by 8192
 constexpr int kTable = 512;       // powers of two
+constexpr int kMarks = 4;         // bounds of a chunk
 
 typedef unsigned long long u64;
 
@@ -63,7 +64,7 @@ struct Args {
   float* prob;
   int chunk, chunks;  // tokens per chunk, chunks per row
   struct ChunkStat* stat;  // [B][chunks]
-  u64* list;               // [B][chunks][kList]: key << 32 | ~index, or kFine masses and kFine / 2 pairs of counts
+  u64* list;               // [B][chunks][kList]: key << 32 | ~index, or kFine masses and counts up to each bin's end
 };
 
 // What a chunk says of itself.
@@ -71,9 +72,15 @@ struct ChunkStat {
   float best, least;  // least: of its finite logits
   int best_at, finite;
   int listed;         // few: tokens on its list (more than kList: it overflowed)
-  uint32_t bound;     // few: at least k tokens reach this key, 0: unknown
+  uint32_t bound[kMarks];  // few: at least mark_of(k, i) tokens reach this key, 0: unknown
   u64 mass;           // in units of its own best
 };
+
+// How many tokens reach a chunk's i-th bound: k, a third of it, a ninth, a 27th.
+__device__ __forceinline__ int mark_of(int k, int i) {
+  for (; i > 0; --i) k = (k + 2) / 3;
+  return k;
+}
 
 constexpr int kNone = 0, kByList = 1, kByBins = 2, kWhole = 3;  // kNone: bad parameters, or greedy
 
@@ -223,8 +230,14 @@ struct Shared {
       u64 few_mass[kFew];
       uint32_t few_at[kFew];
     };
+    struct {
+      double scale[kMaxChunks];  // a chunk's units in the row's
+      float off[kMaxChunks];     // its bins count from here; infinity: it has nothing
+    };
   };
   u64 chunk_mass[kMaxChunks];
+  u64 cum_mass[kFine + 1];       // of the bins up to here; entry 0 is 0
+  int cum_count[kFine + 1];
   int scan_c[kWaves];
   u64 scan_m[kWaves];
   float x[kWaves];
@@ -232,11 +245,12 @@ struct Shared {
   int bin, bc;
   u64 bm;
   int n;
+  uint32_t bound;
 };
 
 // The long way, over the whole row.
 template <bool ALIGNED>
-__device__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Shared& sh) {
+__device__ __forceinline__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Shared& sh) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, V = a.V;
   const float* row = a.logits + (long)b * a.ld;
     Cut cut{0, INT32_MAX, 0, 0};  // everything
@@ -275,10 +289,16 @@ __device__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Sha
         sh.mass[bin] += cut.ties * wg.units(wg.weight(logit_of(cut.key)));
       }
       __syncthreads();
-      const int hi = kBins - 1 - 2 * tid;  // two bins a thread, the largest logits first
-      const int c0 = sh.count[hi], c1 = sh.count[hi - 1];
-      const u64 m0 = sh.mass[hi], m1 = sh.mass[hi - 1];
-      const Scan sc = block_scan(c0 + c1, m0 + m1, sh.scan_c, sh.scan_m);
+      constexpr int kB = kBins / kThreads;
+      const int hi = kBins - 1 - kB * tid;  // some bins a thread, the largest logits first
+      int c0 = 0;
+      u64 m0 = 0;
+#pragma unroll
+      for (int k = 0; k < kB; ++k) {
+        c0 += sh.count[hi - k];
+        m0 += sh.mass[hi - k];
+      }
+      const Scan sc = block_scan(c0, m0, sh.scan_c, sh.scan_m);
       if (level == 0 && (want >= 0 ? sc.ct <= want : !((double)sc.mt >= share))) {  // uniform: everything stays
         cut.count = sc.ct;
         cut.mass = sc.mt;
@@ -286,12 +306,12 @@ __device__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Sha
       }
       if (tid == 0) sh.bin = -1;
       __syncthreads();
-      int bc = above_c + sc.c - c0 - c1;
-      u64 bm = above_m + sc.m - m0 - m1;
+      int bc = above_c + sc.c - c0;
+      u64 bm = above_m + sc.m - m0;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int c = k == 0 ? c0 : c1;
-        const u64 m = k == 0 ? m0 : m1;
+      for (int k = 0; k < kB; ++k) {
+        const int c = sh.count[hi - k];
+        const u64 m = sh.mass[hi - k];
         // the cut's bin: the first whose end reaches it
         const bool before = want >= 0 ? bc < want : (double)bm < share, after = want >= 0 ? bc + c >= want : (double)(bm + m) >= share;
         if (c > 0 && before && after) {
@@ -440,28 +460,29 @@ __device__ void row_cut(const Args& a, const Ask& q, const Weigh& wg, int b, Sha
 __device__ __forceinline__ void fill_table(double* table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = 2.0 * exp_nonpos((i - kTable) * (0.69314718055994530942 / kTable));
 }
-// Units of 2^-shift of exp((x - best) / T), y = (x - best) 512 log2(e) / T: a power of two from the table
-// times 1 + g, g = 2^(r / 512) - 1 in fp32 with |r| <= 1/2, so the weight is within 1e-10 of its own value.
-// Whole units come out of the sum with 2^52.
+// Units of 2^-shift (shift <= 50) of exp((x - best) / T), y = (x - best) 512 log2(e) / T <= 0: a power of two
+// from the table times the series of 2^(r / 512), |r| <= 1/2, whose next term is 1e-14. Rounding to whole
+// numbers is done by adding numbers whose last bit is 1. What is far below one unit comes out 0.
 __device__ __forceinline__ u64 fast_units(double y, int shift, const double* table) {
-  y = fmax(y, -512000.0);
-  const double k = rint(y);
-  const float r = (float)(y - k);
-  const int n = (int)k;
-  constexpr float kL = 0.69314718f / kTable;  // ln 2 / 512
-  const float g = r * fmaf(r, fmaf(r, kL * kL * kL / 6.f, kL * kL / 2.f), kL);
-  const double t = table[n & (kTable - 1)];
-  const double w = ldexp(fma(t, (double)g, t), (n >> 9) + shift);
-  return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;
+  constexpr double kL = 0.69314718055994530942 / kTable, kWhole = 6755399441055744.0;  // 1.5 * 2^52
+  y = fmax(y, -64.0 * kTable);
+  const double z = y + kWhole;
+  const double r = y - (z - kWhole);
+  const int n = (int)(uint32_t)__double_as_longlong(z);
+  const double g = r * fma(r, fma(r, kL * kL * kL / 6.0, kL * kL / 2.0), kL);
+  const double t = __longlong_as_double(__double_as_longlong(table[n & (kTable - 1)]) + ((long long)((n >> 9) + shift) << 52));
+  return (u64)__double_as_longlong(fma(t, g, t) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
 template <bool ALIGNED, int PER>
-__global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
-  constexpr int kW = kChunkThreads / kWave, kSub = 4;  // groups whose maxima bound the k-th token: 4 a thread
+__global__ __launch_bounds__(kChunkThreads, 4) void sample_chunk_kernel(Args a) {
+  constexpr int kW = kChunkThreads / kWave, kSub = 2;  // groups whose maxima bound the k-th token: 2 a thread
+  static_assert(kW == kMarks, "a bound for each wave");
   __shared__ float s_x[kW], s_y[kW];
   __shared__ int s_i[kW], s_f[kW], s_n;
   __shared__ u64 s_m[kW];
-  __shared__ uint32_t s_bound;
+  __shared__ uint32_t s_bound[kMarks];
+  __shared__ int s_c[kW];
   __shared__ union {
     uint32_t sub[kSub * kChunkThreads];
     struct {
@@ -521,9 +542,9 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
   if (q.mode == kByList) {
 #pragma unroll
     for (int k = 0; k < kSub; ++k) {
-      float m = -INFINITY;  // of PER float4s over kSub groups
+      float m = -INFINITY;
 #pragma unroll
-      for (int e = k * PER; e < (k + 1) * PER; ++e) m = fmaxf(m, x[e / 4][e % 4]);
+      for (int e = k * 4 * PER / kSub; e < (k + 1) * 4 * PER / kSub; ++e) m = fmaxf(m, x[e / 4][e % 4]);
       sh.sub[k * kChunkThreads + tid] = key_of(m);
     }
   }
@@ -540,10 +561,11 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
     least = fminf(least, s_y[w]);
     finite += s_f[w];
   }
-  ChunkStat st{best, least, at, finite, 0, 0, 0};
+  ChunkStat st{best, least, at, finite, 0, {}, 0};
   u64* list = a.list + ((size_t)b * a.chunks + c) * kList;
   if (q.mode == kByList) {
-    if (wave == 0) {  // the largest key of 16 bits that k of the groups' maxima reach
+    {  // the largest key of 16 bits that so many of the groups' maxima reach
+      const int want = mark_of(q.top_k, wave);
       uint32_t sub[kSub * kW];
 #pragma unroll
       for (int k = 0; k < kSub * kW; ++k) sub[k] = sh.sub[k * kWave + lane];
@@ -552,12 +574,12 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
         int n = 0;
 #pragma unroll
         for (int k = 0; k < kSub * kW; ++k) n += __popcll(__ballot(sub[k] >= (bound | bit)));
-        if (n >= q.top_k) bound |= bit;
+        if (n >= want) bound |= bit;
       }
-      if (lane == 0) s_bound = bound;
+      if (lane == 0) s_bound[wave] = bound;
     }
     __syncthreads();
-    const uint32_t bound = s_bound;
+    const uint32_t bound = s_bound[0];
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
@@ -570,9 +592,10 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
       }
     __syncthreads();
     st.listed = s_n;
-    st.bound = bound > key_of(-INFINITY) ? bound : 0;
+#pragma unroll
+    for (int i = 0; i < kMarks; ++i) st.bound[i] = s_bound[i] > key_of(-INFINITY) ? s_bound[i] : 0;
   } else if (q.mode != kNone && best > -INFINITY) {
-    const double to = kTable * 1.44269504088896340736 / (double)q.temp, off = -(double)best * to;
+    const double to = kTable * 1.44269504088896340736 / (double)q.temp, from = (double)best;
     const float s = bin_scale(q), top = bin_of(best, s);
     const float last = q.mode == kByBins ? (float)last_bin(q, a.V) : -1.f;
     u64 m = 0;
@@ -580,32 +603,78 @@ __global__ __launch_bounds__(kChunkThreads) void sample_chunk_kernel(Args a) {
     for (int j = 0; j < PER; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const u64 w = fast_units(fma((double)x[j][e], to, off), a.shift, sh.table);
+        const u64 w = fast_units(((double)x[j][e] - from) * to, a.shift, sh.table);
         m += w;
-        const float bin = top - bin_of(x[j][e], s);
-        if (bin <= last) {  // none where bins are not wanted
-          atomicAdd(&sh.mass[(int)bin], w);
-          atomicAdd(&sh.count[(int)bin], 1u);
+        if (q.mode == kByBins) {  // uniform
+          const float bin = top - bin_of(x[j][e], s);
+          if (bin <= last) {
+            atomicAdd(&sh.mass[(int)bin], w);
+            atomicAdd(&sh.count[(int)bin], 1u);
+          }
         }
       }
-    for (int o = 1; o < kWave; o <<= 1) m += (u64)__shfl_xor((unsigned)(m >> 32), o, kWave) << 32 | __shfl_xor((unsigned)m, o, kWave);
+    auto add_up = [&](u64 v) {
+      for (int o = 1; o < kWave; o <<= 1) v += (u64)__shfl_xor((unsigned)(v >> 32), o, kWave) << 32 | __shfl_xor((unsigned)v, o, kWave);
+      return v;
+    };
+    m = add_up(m);
     if (lane == 0) s_m[wave] = m;
     __syncthreads();
     for (int w = 0; w < kW; ++w) st.mass += s_m[w];
-    if (q.mode == kByBins) {
-      list[tid] = sh.mass[tid];
-      reinterpret_cast<uint32_t*>(list + kFine)[tid] = sh.count[tid];
+    if (q.mode == kByBins) {  // sums up to each bin's end
+      u64 cm = sh.mass[tid];
+      int cc = sh.count[tid];
+      for (int o = 1; o < kWave; o <<= 1) {
+        const u64 om = shfl_up64(cm, o);
+        const int oc = __shfl_up(cc, o, kWave);
+        if (lane >= o) {
+          cm += om;
+          cc += oc;
+        }
+      }
+      __syncthreads();
+      if (lane == kWave - 1) {
+        s_m[wave] = cm;
+        s_c[wave] = cc;
+      }
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) {
+        cm += s_m[w];
+        cc += s_c[w];
+      }
+      list[tid] = cm;
+      reinterpret_cast<uint32_t*>(list + kFine)[tid] = cc;
     }
   }
   if (tid == 0) a.stat[(size_t)b * a.chunks + c] = st;
 }
 
-// Sorts n2 (a power of two) values, the largest first.
-__device__ __forceinline__ void sort_down(u64* v, int n2) {
-  for (int size = 2; size <= n2; size <<= 1)
-    for (int step = size >> 1; step > 0; step >>= 1) {
+// Sorts v[0 .. n), the largest first (bitonic; zeros behind them up to a power of two of at least 64).
+// Partners less than 64 apart are a wave's own: they are exchanged between its lanes.
+__device__ __forceinline__ void sort_down(u64* v, int n) {
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  int n2 = kWave;
+  while (n2 < n) n2 <<= 1;
+  for (int i = n + tid; i < n2; i += kThreads) v[i] = 0;
+  __syncthreads();
+  auto in_wave = [&](int s0, int s1) {  // the steps within a wave of sizes s0 .. s1
+    for (int i0 = tid & ~(kWave - 1); i0 < n2; i0 += kThreads) {
+      const int i = i0 + lane;
+      u64 x = v[i];
+      for (int size = s0; size <= s1; size <<= 1)
+        for (int step = min(size, kWave) >> 1; step > 0; step >>= 1) {
+          const u64 y = (u64)__shfl_xor((unsigned)(x >> 32), step, kWave) << 32 | __shfl_xor((unsigned)x, step, kWave);
+          const bool larger = ((i & size) == 0) == ((i & step) == 0);  // keeps the larger one
+          x = (x > y) == larger ? x : y;
+        }
+      v[i] = x;
+    }
+  };
+  in_wave(2, kWave);
+  for (int size = 2 * kWave; size <= n2; size <<= 1) {
+    for (int step = size >> 1; step >= kWave; step >>= 1) {
       __syncthreads();
-      for (int i = threadIdx.x; i < n2 >> 1; i += kThreads) {
+      for (int i = tid; i < n2 >> 1; i += kThreads) {
         const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
         const u64 p = v[lo], r = v[hi];
         if ((p < r) == ((lo & size) == 0)) {
@@ -614,14 +683,10 @@ __device__ __forceinline__ void sort_down(u64* v, int n2) {
         }
       }
     }
+    __syncthreads();
+    in_wave(size, size);
+  }
   __syncthreads();
-}
-__device__ __forceinline__ int pad_and_sort(u64* v, int n) {
-  int n2 = 2;
-  while (n2 < n) n2 <<= 1;
-  for (int i = n + threadIdx.x; i < n2; i += kThreads) v[i] = 0;
-  sort_down(v, n2);
-  return n2;
 }
 
 template <bool ALIGNED>
@@ -641,10 +706,10 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     if (tid == 0) answer(-1, 0, 0.f);
     return;
   }
-  // ---- the row's best, its least finite logit and their number; lists that overflowed; the best bound
+  // ---- the row's best, its least finite logit and their number; lists that overflowed
   float best = -INFINITY, least = INFINITY;
   int at = INT32_MAX, finite = 0;
-  uint32_t bound = 0;
+  bool over = false;
   for (int c = tid; c < a.chunks; c += kThreads) {
     const ChunkStat st = stat[c];
     if (st.best > best || (st.best == best && st.best_at < at)) {
@@ -653,7 +718,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     }
     least = fminf(least, st.least);
     finite += st.finite;
-    if (q.mode == kByList) bound = max(bound, st.listed > kList ? 0xffffffffu : st.bound);
+    over |= q.mode == kByList && st.listed > kList;
   }
   if (a.chunks > 1) {  // uniform
     for (int o = 1; o < kWave; o <<= 1) {
@@ -665,14 +730,14 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       }
       least = fminf(least, __shfl_xor(least, o, kWave));
       finite += __shfl_xor(finite, o, kWave);
-      bound = max(bound, (uint32_t)__shfl_xor((int)bound, o, kWave));
     }
   }
+  over = __ballot(over) != 0;
   if (lane == 0) {
     sh.x[wave] = best;
     sh.i[wave] = at;
     sh.scan_c[wave] = finite;
-    sh.scan_m[wave] = (u64)__float_as_uint(least) << 32 | bound;
+    sh.scan_m[wave] = (u64)__float_as_uint(least) << 32 | (over ? 1 : 0);
   }
   if (tid == 0) {
     sh.n = 0;
@@ -684,7 +749,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   at = sh.i[0];
   finite = sh.scan_c[0];
   least = __uint_as_float((uint32_t)(sh.scan_m[0] >> 32));
-  bound = (uint32_t)sh.scan_m[0];
+  over = (uint32_t)sh.scan_m[0] != 0;
   for (int w = 1; w < nw; ++w) {
     if (sh.x[w] > best || (sh.x[w] == best && sh.i[w] < at)) {
       best = sh.x[w];
@@ -692,7 +757,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     }
     finite += sh.scan_c[w];
     least = fminf(least, __uint_as_float((uint32_t)(sh.scan_m[w] >> 32)));
-    bound = max(bound, (uint32_t)sh.scan_m[w]);
+    over |= (uint32_t)sh.scan_m[w] != 0;
   }
   if (best == -INFINITY || q.greedy) {
     if (tid == 0) {
@@ -705,24 +770,60 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   const double share_u = (double)fminf(fmaxf(q.u, 0.f), 1.f);
   const float s = bin_scale(q), top = bin_of(best, s);
   // infinite logits; lists that overflowed
-  bool longway = best == INFINITY || bound == 0xffffffffu;
+  bool longway = best == INFINITY || over;
   if (q.mode == kByList && !longway) {
-    for (int c = wave; c < a.chunks; c += kWaves) {
-      const int n = stat[c].listed;
-      const u64* list = a.list + ((size_t)b * a.chunks + c) * kList;
-      for (int i = lane; i < n; i += kWave) {
-        const u64 e = list[i];
-        if ((uint32_t)(e >> 32) >= bound) {
-          const int to = atomicAdd(&sh.n, 1);
-          if (to < kSort) sh.sorted[to] = e;
+    if (wave == 0) {
+      // The largest key that k tokens of the row are known to reach: the chunks' bounds say how many of
+      // theirs do
+      uint32_t bound = 0;
+      int weight[kMarks];
+#pragma unroll
+      for (int i = 0; i < kMarks; ++i) weight[i] = mark_of(q.top_k, i) - (i + 1 < kMarks ? mark_of(q.top_k, i + 1) : 0);
+      const bool one = a.chunks <= kWave;
+      uint32_t mine[kMarks] = {0, 0, 0, 0};
+      if (one && lane < a.chunks)
+#pragma unroll
+        for (int i = 0; i < kMarks; ++i) mine[i] = stat[lane].bound[i];
+      for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        int n = 0;
+        for (int c0 = 0; c0 < a.chunks; c0 += kWave) {
+          if (!one) {
+#pragma unroll
+            for (int i = 0; i < kMarks; ++i) mine[i] = c0 + lane < a.chunks ? stat[c0 + lane].bound[i] : 0;
+          }
+#pragma unroll
+          for (int i = 0; i < kMarks; ++i) n += weight[i] * __popcll(__ballot(mine[i] >= (bound | bit)));
         }
+        if (n >= q.top_k) bound |= bit;
       }
+      if (lane == 0) sh.bound = bound;
+    }
+    __syncthreads();
+    const uint32_t bound = sh.bound;
+    for (int c0 = wave; c0 < a.chunks; c0 += 4 * kWaves) {  // four lists' first entries at once
+      u64 e[4];
+      int n[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = min(c0 + k * kWaves, a.chunks - 1);
+        n[k] = c0 + k * kWaves < a.chunks ? stat[c].listed : 0;
+        e[k] = a.list[((size_t)b * a.chunks + c) * kList + lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        for (int i = lane; i < n[k]; i += kWave) {
+          const u64 x = i == lane ? e[k] : a.list[((size_t)b * a.chunks + c0 + k * kWaves) * kList + i];
+          if ((uint32_t)(x >> 32) >= bound) {
+            const int to = atomicAdd(&sh.n, 1);
+            if (to < kSort) sh.sorted[to] = x;
+          }
+        }
     }
     __syncthreads();
     const int n = sh.n;
     longway = n > kSort;
     if (!longway) {
-      pad_and_sort(sh.sorted, n);
+      sort_down(sh.sorted, n);
       // the first k, their masses in order, and how many of them stay
       double w = 0.0;
       const u64 mine = tid < min(n, q.top_k) ? sh.sorted[tid] : 0;
@@ -750,38 +851,80 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   // Beside the best a token may weigh nothing although its chunk counted it, and bins have to be exact.
   if (((double)best - (double)least) * wg.inv_t > 690.0 || !(fabsf(top) < 8388608.f) || !(fabsf(bin_of(least, s)) < 8388608.f)) longway = true;
   // a mass in units of a chunk's best, in the row's
-  auto scaled = [&](u64 m, float from) { return (u64)rint((double)m * exp_nonpos(((double)from - (double)best) * wg.inv_t)); };
-  auto bins_of = [&](int c) { return a.list + ((size_t)b * a.chunks + c) * kList; };
+  auto scaled = [&](u64 m, int c) { return (u64)rint((double)m * sh.scale[c]); };
+  if (!longway && q.mode != kByList) {
+    __syncthreads();
+    for (int c = tid; c < a.chunks; c += kThreads) {
+      const float from = stat[c].best;
+      const bool has = from > -INFINITY;
+      sh.off[c] = has ? top - bin_of(from, s) : INFINITY;
+      sh.scale[c] = has ? exp_nonpos(((double)from - (double)best) * wg.inv_t) : 0.0;
+    }
+    __syncthreads();
+  }
+  const u64* sums = a.list + (size_t)b * a.chunks * kList;
+  // the mass of chunk c up to the end of its bin j
+  auto mass_to = [&](int c, float j) { return j >= 0.f ? scaled(sums[(size_t)c * kList + (int)j], c) : 0; };
   u64 cutoff = 0;        // tokens whose (key, ~index) reaches this stay
   int kept = finite;
   int lo = 0, hi = -1;   // the bins whose tokens are in sh.sorted; the bins in front of them stay whole
   if (q.mode == kByBins && !longway) {
     const int last = last_bin(q, V);
-    u64 fm = 0, total = 0;
-    int fc = 0;
-    for (int c = tid; c < a.chunks; c += kThreads)
-      if (stat[c].best > -INFINITY) total += scaled(stat[c].mass, stat[c].best);
+    u64 total = 0;
+    for (int c = tid; c < a.chunks; c += kThreads) total += scaled(stat[c].mass, c);
     total = block_scan(0, total, sh.scan_c, sh.scan_m).mt;
-    if (tid <= last)
-      for (int c = 0; c < a.chunks; ++c) {
-        const float from = stat[c].best, j = (float)tid - (top - bin_of(from, s));
-        if (!(from > -INFINITY) || !(j >= 0.f)) continue;
-        const u64 m = bins_of(c)[(int)j];
-        if (m != 0) fm += scaled(m, from);
-        fc += (int)reinterpret_cast<const uint32_t*>(bins_of(c) + kFine)[(int)j];
+    {  // half of the threads each take every second chunk of a bin
+      static_assert(kThreads == 2 * kFine, "two threads a bin");
+      constexpr int kAhead = 8;
+      const int bin = tid & (kFine - 1);
+      u64 m = 0;
+      int n = 0;
+      for (int c0 = tid / kFine; c0 < a.chunks; c0 += 2 * kAhead) {
+        u64 pm[kAhead];
+        int pn[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = min(c0 + 2 * k, a.chunks - 1), j = max((int)fmaxf((float)bin - sh.off[c], -1.f), 0);
+          pm[k] = sums[(size_t)c * kList + j];
+          pn[k] = (int)reinterpret_cast<const uint32_t*>(sums + (size_t)c * kList + kFine)[j];
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = c0 + 2 * k;
+          if (c < a.chunks && (float)bin - sh.off[c] >= 0.f) {
+            m += scaled(pm[k], c);
+            n += pn[k];
+          }
+        }
       }
-    const Scan sc = block_scan(fc, fm, sh.scan_c, sh.scan_m);
+      if (tid == 0) {
+        sh.cum_mass[0] = 0;
+        sh.cum_count[0] = 0;
+      }
+      if (tid < kFine) {
+        sh.cum_mass[bin + 1] = m;
+        sh.cum_count[bin + 1] = n;
+      }
+      __syncthreads();
+      if (tid >= kFine) {
+        sh.cum_mass[bin + 1] += m;
+        sh.cum_count[bin + 1] += n;
+      }
+      __syncthreads();
+    }
     int above_c = 0;  // tokens and mass in front of bin lo
     u64 above = 0;
     // The first bin whose end reaches `want` tokens (want > 0) or `share` units; -1: none.
     auto find = [&](int want, double share) {
-      __syncthreads();
       if (tid == 0) sh.bin = -1;
       __syncthreads();
-      const bool hit = want > 0 ? sc.c - fc < want && sc.c >= want : (double)(sc.m - fm) < share && (double)sc.m >= share;
-      if (tid <= last && fc > 0 && hit) sh.bin = tid;
+      if (tid <= last && (want > 0 ? sh.cum_count[tid] < want && sh.cum_count[tid + 1] >= want
+                                   : (double)sh.cum_mass[tid] < share && (double)sh.cum_mass[tid + 1] >= share))
+        sh.bin = tid;
       __syncthreads();
-      return sh.bin;
+      const int bin = sh.bin;
+      __syncthreads();
+      return bin;
     };
     // Bins b0 .. b1 into sh.sorted. false: too many tokens.
     auto gather = [&](int b0, int b1) {
@@ -790,23 +933,19 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       hi = b1;
       __syncthreads();
       if (tid == 0) sh.n = 0;
-      if (tid == b0) {
-        sh.bc = sc.c - fc;
-        sh.bm = sc.m - fm;
-      }
       __syncthreads();
-      above_c = sh.bc;
-      above = sh.bm;
+      above_c = sh.cum_count[b0];
+      above = sh.cum_mass[b0];
+      constexpr int kAhead = 8;
       for (int c = wave; c < a.chunks; c += kWaves) {
-        const float from = stat[c].best;
-        if (!(from > -INFINITY) || top - bin_of(from, s) > (float)b1) continue;
+        if (!(sh.off[c] <= (float)b1)) continue;
         const int end = min(V, (c + 1) * a.chunk);
-        for (int v0 = c * a.chunk + 4 * lane; v0 < end; v0 += 16 * kWave) {
-          float x[4][4];
+        for (int v0 = c * a.chunk + 4 * lane; v0 < end; v0 += 4 * kAhead * kWave) {
+          float x[kAhead][4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) load4<ALIGNED>(row, v0 + 4 * k * kWave < end ? V : 0, v0 + 4 * k * kWave, x[k]);
+          for (int k = 0; k < kAhead; ++k) load4<ALIGNED>(row, v0 + 4 * k * kWave < end ? V : 0, v0 + 4 * k * kWave, x[k]);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
+          for (int k = 0; k < 4 * kAhead; ++k) {
             const float y = x[k >> 2][k & 3], bin = top - bin_of(y, s);
             if (bin >= (float)b0 && bin <= (float)b1) {  // no NaN, no infinity
               const int to = atomicAdd(&sh.n, 1);
@@ -817,7 +956,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       }
       __syncthreads();
       if (sh.n > kSort) return false;
-      pad_and_sort(sh.sorted, sh.n);
+      sort_down(sh.sorted, sh.n);
       return true;
     };
     // How many of the first `most` tokens of sh.sorted stay, by weight (floor_w > 0) or by the mass in front.
@@ -851,29 +990,20 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     const float xm = q.min_p > 0.f ? (float)((double)best + (double)q.temp * log((double)q.min_p)) : -INFINITY;
     const float edge = fmaxf(top - bin_of(xm, s), 0.f);
     const bool by_m = edge < (float)last;  // else behind the bins: it cuts nothing that another cut leaves
-    bool cut = q.top_k > 0;
-    if (q.top_p < 1.f && !longway) {
-      const double share = (double)q.top_p * (double)total;
-      const int bin = find(0, share);
-      if (bin < 0) {
-        longway = !by_m;  // behind the bins
-      } else if (!gather(bin, bin)) {
+    const int m0 = max((int)fminf(edge, (float)last) - 1, 0), m1 = min((int)fminf(edge, (float)last) + 1, last);
+    const int pbin = q.top_p < 1.f && !longway ? find(0, (double)q.top_p * (double)total) : -1;
+    // p cuts in front of all that m may cut, m in front of p's bin, or both in one range of bins
+    const bool only_p = pbin >= 0 && (!by_m || pbin < m0), only_m = by_m && (pbin < 0 || m1 < pbin);
+    // a cut that lies behind the bins, and none in front of it
+    if (cutoff == 0 && (q.top_p < 1.f || q.min_p > 0.f) && pbin < 0 && !by_m) longway = true;
+    if (!longway && (pbin >= 0 || by_m)) {
+      const int g0 = only_p ? pbin : only_m ? m0 : min(pbin, m0), g1 = only_p ? pbin : only_m ? m1 : max(pbin, m1);
+      if (!gather(g0, g1)) {
         longway = true;
       } else {
-        cut = true;
-        const int n = within(share, 0.0, min(sh.n, kept - above_c));
-        if (n > 0 && above_c + n < kept) {
-          kept = above_c + n;
-          cutoff = sh.sorted[n - 1];
-        }
-      }
-    }
-    if (q.min_p > 0.f && !by_m && !cut) longway = true;
-    if (by_m && !longway) {
-      if (!gather(max((int)edge - 1, 0), (int)edge + 1)) {
-        longway = true;
-      } else {
-        const int n = within(0.0, (double)q.min_p, sh.n);
+        int n = max(min(sh.n, kept - above_c), 0);
+        if (!only_m) n = min(n, within((double)q.top_p * (double)total, 0.0, n));
+        if (!only_p) n = min(n, within(0.0, (double)q.min_p, n));
         if (above_c + n < kept) {
           kept = above_c + n;
           cutoff = n > 0 ? sh.sorted[n - 1] : sh.n > 0 ? sh.sorted[0] + 1 : (u64)key_of(xm) << 32;
@@ -891,23 +1021,8 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     return;
   }
   // ---- the chunks' kept masses, the chunk of the draw
-  for (int c = wave; c < a.chunks; c += kWaves) {
-    const float from = stat[c].best;
-    u64 m = 0;
-    if (from > -INFINITY) {
-      if (cutoff == 0) {
-        m = lane == 0 ? scaled(stat[c].mass, from) : 0;
-      } else {
-        const int off = (int)(top - bin_of(from, s));  // its bins count from here
-        for (int bin = off + lane; bin < lo; bin += kWave) {
-          const u64 k = bins_of(c)[bin - off];
-          if (k != 0) m += scaled(k, from);
-        }
-      }
-    }
-    for (int o = 1; o < kWave; o <<= 1) m += (u64)__shfl_xor((unsigned)(m >> 32), o, kWave) << 32 | __shfl_xor((unsigned)m, o, kWave);
-    if (lane == 0) sh.chunk_mass[c] = m;
-  }
+  for (int c = tid; c < a.chunks; c += kThreads)
+    sh.chunk_mass[c] = cutoff == 0 ? scaled(stat[c].mass, c) : mass_to(c, (float)(lo - 1) - sh.off[c]);
   __syncthreads();
   if (cutoff != 0)
     for (int i = tid; i < sh.n; i += kThreads) {
