@@ -940,39 +940,117 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       for (int c = wave; c < a.chunks; c += kWaves) {
         if (!(sh.off[c] <= (float)b1)) continue;
         const int end = min(V, (c + 1) * a.chunk);
-        for (int v0 = c * a.chunk + 4 * lane; v0 < end; v0 += 4 * kAhead * kWave) {
+        for (int v0 = c * a.chunk + 4 * lane; v0 - 4 * lane < end; v0 += 4 * kAhead * kWave) {  // whole waves
           float x[kAhead][4];
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) load4<ALIGNED>(row, v0 + 4 * k * kWave < end ? V : 0, v0 + 4 * k * kWave, x[k]);
+          uint32_t hits = 0;
+          static_assert(4 * kAhead == 32, "a bit for each");
 #pragma unroll
           for (int k = 0; k < 4 * kAhead; ++k) {
             const float y = x[k >> 2][k & 3], bin = top - bin_of(y, s);
-            if (bin >= (float)b0 && bin <= (float)b1) {  // no NaN, no infinity
-              const int to = atomicAdd(&sh.n, 1);
-              if (to < kSort) sh.sorted[to] = (u64)key_of(y) << 32 | ~(uint32_t)(v0 + (k >> 2) * 4 * kWave + (k & 3));
-            }
+            if (bin >= (float)b0 && bin <= (float)b1) hits |= 1u << k;  // no NaN, no infinity
           }
+          const int mine = __popc(hits);
+          int upto = mine;
+          for (int o = 1; o < kWave; o <<= 1) {
+            const int t = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += t;
+          }
+          int to = 0;
+          if (lane == kWave - 1 && upto > 0) to = atomicAdd(&sh.n, upto);
+          to = __shfl(to, kWave - 1, kWave) + upto - mine;
+#pragma unroll
+          for (int k = 0; k < 4 * kAhead; ++k)
+            if ((hits >> k & 1u) != 0) {
+              if (to < kSort) sh.sorted[to] = (u64)key_of(x[k >> 2][k & 3]) << 32 | ~(uint32_t)(v0 + (k >> 2) * 4 * kWave + (k & 3));
+              ++to;
+            }
         }
       }
       __syncthreads();
-      if (sh.n > kSort) return false;
-      sort_down(sh.sorted, sh.n);
-      return true;
+      return sh.n <= kSort;
     };
-    // How many of the first `most` tokens of sh.sorted stay, by weight (floor_w > 0) or by the mass in front.
-    auto within = [&](double share, double floor_w, int most) {
-      int n = 0;
-      u64 run = above;
-      for (int i0 = 0; i0 < most; i0 += kThreads) {
-        const int i = i0 + tid;
-        const double w = i < most ? wg.weight(logit_of((uint32_t)(sh.sorted[i] >> 32))) : 0.0;
-        const u64 m = wg.units(w);
-        const Scan t = block_scan(0, m, sh.scan_c, sh.scan_m);
-        const bool stays = i < most && (floor_w > 0.0 ? w >= floor_w : (double)(run + t.m - m) < share);
-        n += block_scan(stays ? 1 : 0, 0, sh.scan_c, sh.scan_m).ct;
-        run += t.mt;
+    // The last of the gathered tokens (in order) that stays and how many do, by count (want > 0: of them) or by
+    // the mass in front (share): counts and masses by 256 steps of the keys, then the tokens of the step
+    // that holds the cut, sorted.
+    auto select = [&](int want, double share, u64& at) {
+      u64* const mass = sh.chunk_mass;  // not in use yet
+      uint32_t* const count = reinterpret_cast<uint32_t*>(sh.chunk_mass + kFine);
+      u64* const small = sh.chunk_mass + 2 * kFine;
+      constexpr int kSmall = kMaxChunks - 2 * kFine;
+      const int n = sh.n;
+      uint32_t least = 0xffffffffu, most = 0;
+      for (int i = tid; i < n; i += kThreads) {
+        const uint32_t key = (uint32_t)(sh.sorted[i] >> 32);
+        least = min(least, key);
+        most = max(most, key);
       }
-      return n;
+      for (int o = 1; o < kWave; o <<= 1) {
+        least = min(least, (uint32_t)__shfl_xor((int)least, o, kWave));
+        most = max(most, (uint32_t)__shfl_xor((int)most, o, kWave));
+      }
+      if (lane == 0) sh.scan_m[wave] = (u64)most << 32 | least;
+      if (tid < kFine) {
+        mass[tid] = 0;
+        count[tid] = 0;
+      }
+      if (tid == 0) sh.bc = -1;
+      __syncthreads();
+      for (int w = 0; w < kWaves; ++w) {
+        least = min(least, (uint32_t)sh.scan_m[w]);
+        most = max(most, (uint32_t)(sh.scan_m[w] >> 32));
+      }
+      const int bits = max(32 - __clz((int)(most - least)), 8) - 8;  // the keys' range in 256 steps
+      for (int i = tid; i < n; i += kThreads) {
+        const uint32_t key = (uint32_t)(sh.sorted[i] >> 32);
+        atomicAdd(&count[(most - key) >> bits], 1u);
+        if (want == 0) atomicAdd(&mass[(most - key) >> bits], wg.units(wg.weight(logit_of(key))));
+      }
+      __syncthreads();
+      const int c = tid < kFine ? (int)count[tid] : 0;
+      const u64 m = tid < kFine ? mass[tid] : 0;
+      const Scan sc = block_scan(c, m, sh.scan_c, sh.scan_m);
+      const bool holds = want > 0 ? sc.c - c < want && sc.c >= want : (double)(above + sc.m - m) < share && ((double)(above + sc.m) >= share || sc.c == n);
+      if (c > 0 && holds) {
+        sh.bc = tid;
+        sh.bin = sc.c - c;
+        sh.bm = above + sc.m - m;
+      }
+      __syncthreads();
+      const int step = sh.bc, front = sh.bin, here = step < 0 ? 0 : (int)count[step];
+      const u64 ahead = sh.bm;
+      if (step < 0) return 0;
+      __syncthreads();
+      u64* list = small;
+      if (here <= kSmall / 2) {  // the sort wants a power of two
+        if (tid == 0) sh.bin = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads)
+          if ((int)((most - (uint32_t)(sh.sorted[i] >> 32)) >> bits) == step) small[atomicAdd(&sh.bin, 1)] = sh.sorted[i];
+        __syncthreads();
+        sort_down(small, here);
+      } else {  // crowded (ties): all of them in order, those of the step behind the ones in front
+        sort_down(sh.sorted, n);
+        list = sh.sorted + front;
+      }
+      int stay = 0;
+      if (want > 0) {
+        stay = want - front;
+      } else {
+        u64 run = ahead;
+        for (int i0 = 0; i0 < here; i0 += kThreads) {
+          const int i = i0 + tid;
+          const u64 w = i < here ? wg.units(wg.weight(logit_of((uint32_t)(list[i] >> 32)))) : 0;
+          const Scan t = block_scan(0, w, sh.scan_c, sh.scan_m);
+          stay += block_scan(i < here && (double)(run + t.m - w) < share ? 1 : 0, 0, sh.scan_c, sh.scan_m).ct;
+          run += t.mt;
+        }
+        stay = max(stay, 1);
+      }
+      at = list[stay - 1];
+      __syncthreads();
+      return front + stay;
     };
     if (q.top_k > 0 && finite > q.top_k) {
       const int bin = find(q.top_k, 0.0);
@@ -980,9 +1058,10 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
         longway = true;
       } else {
         kept = q.top_k;
-        cutoff = sh.sorted[kept - above_c - 1];
+        select(kept - above_c, 0.0, cutoff);
         u64 m = 0;
-        for (int i = tid; i < kept - above_c; i += kThreads) m += wg.units(wg.weight(logit_of((uint32_t)(sh.sorted[i] >> 32))));
+        for (int i = tid; i < sh.n; i += kThreads)
+          if (sh.sorted[i] >= cutoff) m += wg.units(wg.weight(logit_of((uint32_t)(sh.sorted[i] >> 32))));
         total = above + block_scan(0, m, sh.scan_c, sh.scan_m).mt;
       }
     }
@@ -1001,12 +1080,41 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       if (!gather(g0, g1)) {
         longway = true;
       } else {
-        int n = max(min(sh.n, kept - above_c), 0);
-        if (!only_m) n = min(n, within((double)q.top_p * (double)total, 0.0, n));
-        if (!only_p) n = min(n, within(0.0, (double)q.min_p, n));
-        if (above_c + n < kept) {
-          kept = above_c + n;
-          cutoff = n > 0 ? sh.sorted[n - 1] : sh.n > 0 ? sh.sorted[0] + 1 : (u64)key_of(xm) << 32;
+        if (!only_m) {
+          u64 at = 0;
+          const int n = select(0, (double)q.top_p * (double)total, at);
+          if (n > 0 && above_c + n < kept) {
+            kept = above_c + n;
+            cutoff = at;
+          }
+        }
+        if (!only_p) {  // the tokens that weigh enough, and the last of them
+          int n = 0;
+          u64 at = ~0ull;
+          for (int i = tid; i < sh.n; i += kThreads) {
+            const u64 e = sh.sorted[i];
+            if (wg.weight(logit_of((uint32_t)(e >> 32))) >= (double)q.min_p) {
+              ++n;
+              at = min(at, e);
+            }
+          }
+          for (int o = 1; o < kWave; o <<= 1) at = min(at, (u64)__shfl_xor((unsigned)(at >> 32), o, kWave) << 32 | __shfl_xor((unsigned)at, o, kWave));
+          n = block_scan(n, 0, sh.scan_c, sh.scan_m).ct;
+          __syncthreads();
+          if (lane == 0) sh.scan_m[wave] = at;
+          __syncthreads();
+          for (int w = 0; w < kWaves; ++w) at = min(at, sh.scan_m[w]);
+          __syncthreads();
+          if (above_c + n < kept) {
+            kept = above_c + n;
+            if (n > 0) {
+              cutoff = at;
+            } else {  // none: everything above the gathered bins stays
+              u64 most = 0;
+              for (int i = 0; i < sh.n; ++i) most = max(most, sh.sorted[i]);
+              cutoff = sh.n > 0 ? most + 1 : (u64)key_of(xm) << 32;
+            }
+          }
         }
       }
     }
