@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -513,23 +514,34 @@ def sirius_kv_rollback(cache_pos, accept_len, n, *, stream=None):
 
 
 # ---------------------------------------------------------------- the batched serving step
+#
+# A decoding step makes these calls for every layer, with kernels of a few microseconds behind them, so the
+# binding's own time counts: torch's names are looked up once, devices are compared by number, and the structs
+# of include/sirius.h are packed as bytes (0.3 us; a ctypes Structure takes 1.5).
 
-class _RotationC(ctypes.Structure):
-    """struct sirius_rotation of include/sirius.h."""
-    _fields_ = [(n, ctypes.c_void_p) for n in ("freqs", "q_weight", "k_weight")] + \
-               [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("mscale", _F), ("norm_eps", _F)]
-
-
-class _PagedC(ctypes.Structure):
-    """struct sirius_paged of include/sirius.h."""
-    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "cache_pos", "tok_start")] + \
-               [(n, ctypes.c_int) for n in ("B", "T", "max_n", "n_kv_heads", "head_dim", "n_pages", "page_size",
-                                            "max_pages")]
+_ROTATION = struct.Struct("@PPPiiff")  # struct sirius_rotation: freqs, weights, rot_dim, interleaved, mscale, norm_eps
+_PAGED = struct.Struct("@PPPPPiiiiiiii")  # struct sirius_paged: five pointers, B, T, max_n, heads, head size, pages, rows, columns
 
 
-def _elsewhere(t):
-    """Whether t lives on another GPU than torch's current one."""
-    return t.is_cuda and t.device.index != _torch().cuda.current_device()
+class _Names:
+    """torch's names that the calls below use, looked up at the first of them."""
+
+    def __init__(self):
+        torch = _torch()
+        self.f32, self.bf16, self.f64, self.i32, self.i64 = (torch.float32, torch.bfloat16, torch.float64, torch.int32,
+                                                             torch.int64)
+        self.empty = torch.empty
+        self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+_names = None
+
+
+def _bound():
+    global _names
+    if _names is None:
+        _names = _Names()
+    return _names
 
 
 def _there(t, entry, args: dict):
@@ -538,47 +550,59 @@ def _there(t, entry, args: dict):
         return entry(**args)
 
 
-def _dtype(t) -> int:
-    torch = _torch()
-    if t.dtype is torch.float32:
+def _type_of(t, n) -> int:
+    d = t.dtype
+    if d is n.f32:
         return SIRIUS_F32
-    _need(t.dtype is torch.bfloat16, "tensors must be fp32 or bf16")
+    _need(d is n.bf16, "tensors must be fp32 or bf16")
     return SIRIUS_BF16
 
 
 def _rows(t, name):
     """(tokens, heads, head size, elements between tokens) of [T, heads, hd] whose tokens may be apart."""
-    _need(t.dim() == 3, f"{name} must be [T, heads, head_dim]")
-    n, h, d = t.shape
-    s = t.stride()
-    _need(t.is_cuda, "tensors must live on the GPU")
-    _need(n == 0 or (s[2] == 1 and (h == 1 or s[1] == d)), f"the heads of a token of {name} must be contiguous")
-    return n, h, d, s[0] if n > 1 else h * d
+    shape = t.shape
+    _need(len(shape) == 3, f"{name} must be [T, heads, head_dim]")
+    n, h, d = shape
+    if n > 1 or not t.is_contiguous():
+        s = t.stride()
+        _need(n == 0 or (s[2] == 1 and (h == 1 or s[1] == d)), f"the heads of a token of {name} must be contiguous")
+        if n > 1:
+            return n, h, d, s[0]
+    return n, h, d, h * d
 
 
-def _same_device(first, *ts):
+def _on_gpu(dev: int, *ts):
+    """Every tensor (or None) on this GPU."""
+    _need(dev >= 0, "tensors must live on the GPU")
     for t in ts:
-        _need(t is None or t.device == first.device, "tensors must live on one GPU")
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must live on one GPU")
 
 
-def _int32(t, shape, name):
-    _need(t.dtype is _torch().int32 and tuple(t.shape) == shape and t.is_contiguous(),
-          f"{name} must be int32 {list(shape)}, contiguous")
+def _vector(t, dtype, size, name):
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != size or not t.is_contiguous():
+        raise ValueError(f"{name} must be {dtype} [{size}], contiguous")
 
 
-def _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd):
-    torch = _torch()
-    half = 0
+def _like(out, t, dtype, name):
+    if out.dtype is not dtype or out.shape != t.shape or not out.is_contiguous():
+        raise ValueError(f"{name} must be {dtype} {list(t.shape)}, contiguous")
+
+
+def _rotation(n, freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd):
+    half = f = qw = kw = 0
     if freqs is not None:
-        _need(freqs.dtype is torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and 2 * freqs.numel() <= hd,
-              "freqs must be float64 [rot_dim / 2], rot_dim at most head_dim")
         half = freqs.numel()
-    for w in (q_weight, k_weight):
-        if w is not None:
-            _need(w.dtype is torch.bfloat16 and tuple(w.shape) == (hd,) and w.is_contiguous(),
-                  "norm weights must be bf16 [head_dim]")
-    return _RotationC(_ptr(freqs) if half else None, _ptr(q_weight), _ptr(k_weight), 2 * half, 1 if interleaved else 0,
-                      mscale, norm_eps)
+        _need(freqs.dtype is n.f64 and freqs.dim() == 1 and freqs.is_contiguous() and 2 * half <= hd,
+              "freqs must be float64 [rot_dim / 2], rot_dim at most head_dim")
+        f = freqs.data_ptr() if half else 0
+    if q_weight is not None:
+        _vector(q_weight, n.bf16, hd, "q_weight")
+        qw = q_weight.data_ptr()
+    if k_weight is not None:
+        _vector(k_weight, n.bf16, hd, "k_weight")
+        kw = k_weight.data_ptr()
+    return _ROTATION.pack(f, qw, kw, 2 * half, 1 if interleaved else 0, mscale, norm_eps)
 
 
 _ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "smooth": 3, "ramp": 4}
@@ -604,63 +628,74 @@ def sirius_rope(q, k, positions, freqs, *, interleaved=False, mscale=1.0, norm_e
     k_out bf16), contiguous, or None in the place of an absent input."""
     if stream is not None:
         return _on(stream, sirius_rope, locals())
-    _need(q is not None or k is not None, "q and k are both None")
-    first = q if q is not None else k
-    if _elsewhere(first):
+    if q is None and k is None:
+        raise ValueError("q and k are both None")
+    names = _names or _bound()
+    dev = (k if q is None else q).get_device()
+    if dev >= 0 and dev != names.current():
         args = dict(locals())
-        del args["first"]
-        return _there(first, sirius_rope, args)
-    torch = _torch()
-    t, h, hkv, hd, ldq, ldk = int(first.shape[0]), 1, 1, int(first.shape[-1]), 0, 0
-    qt = kt = SIRIUS_F32
+        del args["names"], args["dev"]
+        return _there(k if q is None else q, sirius_rope, args)
+    _on_gpu(dev, k, positions, freqs, q_weight, k_weight, q_out, k_out)
+    h = hkv = 1
+    ldq = ldk = qt = kt = qp = kp = qo = ko = 0
     if q is not None:
         t, h, hd, ldq = _rows(q, "q")
-        qt = _dtype(q)
+        qt = _type_of(q, names)
         if q_out is None:
-            q_out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
-        _need(q_out.dtype is q.dtype and q_out.shape == q.shape and q_out.is_contiguous(),
-              "q_out must be like q, contiguous")
+            q_out = names.empty((t, h, hd), dtype=q.dtype, device=q.device)
+        else:
+            _like(q_out, q, q.dtype, "q_out")
+        qp, qo = q.data_ptr(), q_out.data_ptr()
     else:
         q_out = None
     if k is not None:
         tk, hkv, dk, ldk = _rows(k, "k")
         _need(q is None or (tk == t and dk == hd), "q and k disagree on T or head_dim")
-        kt = _dtype(k)
+        t, hd = tk, dk
+        kt = _type_of(k, names)
         if k_out is None:
-            k_out = torch.empty((tk, hkv, dk), dtype=torch.bfloat16, device=k.device)
-        _need(k_out.dtype is torch.bfloat16 and k_out.shape == k.shape and k_out.is_contiguous(),
-              "k_out must be bf16 [T, Hkv, head_dim], contiguous")
+            k_out = names.empty((tk, hkv, dk), dtype=names.bf16, device=k.device)
+        else:
+            _like(k_out, k, names.bf16, "k_out")
+        kp, ko = k.data_ptr(), k_out.data_ptr()
     else:
         k_out = None
-    _int32(positions, (t,), "positions")
-    _same_device(first, k, positions, freqs, q_weight, k_weight, q_out, k_out)
-    rot = _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
-    _check(lib().sirius_rope(_ptr(q), qt, ldq, _ptr(k), kt, ldk, _ptr(positions), t, h, hkv, hd, ctypes.byref(rot),
-                             _ptr(q_out), _ptr(k_out), _handle()))
+    _vector(positions, names.i32, t, "positions")
+    rot = _rotation(names, freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
+    rc = (_lib or lib()).sirius_rope(qp, qt, ldq, kp, kt, ldk, positions.data_ptr(), t, h, hkv, hd, rot, qo, ko, _handle())
+    if rc:
+        _check(rc)
     return q_out, k_out
 
 
-def _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n):
-    """The call's sirius_paged: T tokens of head size hd, max_n of a sequence at most (None: T, or T / B)."""
-    torch = _torch()
-    _need(k_pages.dtype is torch.bfloat16 and v_pages.dtype is torch.bfloat16 and k_pages.dim() == 4 and v_pages.dim() == 4
-          and k_pages.is_contiguous() and v_pages.is_contiguous(), "k_pages and v_pages must be contiguous bf16 [pages, ...]")
+def _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n):
+    """The call's sirius_paged as bytes, for T tokens of head size hd, and its B, max_n and number of heads (max_n None: T, or
+    T / B without tok_start)."""
     pages, hkv, size, d = k_pages.shape
-    _need(d == hd and v_pages.shape == (pages, hkv, d, size),
-          "pages must be [pages, Hkv, page_size, head_dim] (keys) and [pages, Hkv, head_dim, page_size] (values)")
-    _need(page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(),
-          "page_table must be int32 [B, pages per sequence], contiguous")
+    if k_pages.dtype is not names.bf16 or v_pages.dtype is not names.bf16 or not k_pages.is_contiguous() or not v_pages.is_contiguous():
+        raise ValueError("k_pages and v_pages must be contiguous bf16 [pages, ...]")
+    if d != hd or v_pages.shape != (pages, hkv, d, size):
+        raise ValueError("pages must be [pages, Hkv, page_size, head_dim] (keys) and [pages, Hkv, head_dim, page_size] (values)")
+    if page_table.dtype is not names.i32 or page_table.dim() != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be int32 [B, pages per sequence], contiguous")
     bsz, wide = page_table.shape
-    _int32(cache_pos, (bsz,), "cache_pos")
+    _vector(cache_pos, names.i32, bsz, "cache_pos")
+    start = 0
     if tok_start is not None:
-        _int32(tok_start, (bsz + 1,), "tok_start")
+        _vector(tok_start, names.i32, bsz + 1, "tok_start")
+        start = tok_start.data_ptr()
         n = t if max_n is None else int(max_n)
     else:
         _need(bsz == 0 or t % bsz == 0, "without tok_start every sequence has T / B tokens")
         n = t // bsz if bsz else 0
         _need(max_n is None or max_n >= n, "max_n is less than T / B")
-    return _PagedC(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_pos), _ptr(tok_start), bsz, t, n, hkv, d,
-                   pages, size, wide)
+    return _PAGED.pack(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), cache_pos.data_ptr(), start, bsz, t, n, hkv,
+                       d, pages, size, wide), bsz, n, hkv
+
+
+def _four(t, name):
+    _need(t.dim() == 4, f"{name} must be [pages, heads, ...], four dimensions")
 
 
 def sirius_kv_append(q, k, v, k_pages, v_pages, page_table, cache_pos, freqs=None, *, tok_start=None, positions=None,
@@ -671,31 +706,40 @@ def sirius_kv_append(q, k, v, k_pages, v_pages, page_table, cache_pos, freqs=Non
     [B + 1] or None (T / B tokens each), positions [T] or None (the cache rows): int32. Returns q_out."""
     if stream is not None:
         return _on(stream, sirius_kv_append, locals())
-    if _elsewhere(k):
-        return _there(k, sirius_kv_append, locals())
-    torch = _torch()
+    names = _names or _bound()
+    dev = k.get_device()
+    if dev >= 0 and dev != names.current():
+        args = dict(locals())
+        del args["names"], args["dev"]
+        return _there(k, sirius_kv_append, args)
+    _on_gpu(dev, q, v, k_pages, v_pages, page_table, cache_pos, tok_start, positions, freqs, q_weight, k_weight, q_out)
     t, hkv, hd, ldk = _rows(k, "k")
     tv, hv, dv, ldv = _rows(v, "v")
     _need(tv == t and hv == hkv and dv == hd and v.dtype is k.dtype, "k and v must be alike")
-    _need(hkv == k_pages.shape[1], "k and the pages disagree on the number of heads")
-    h, ldq, qt = 1, 0, SIRIUS_F32
+    _four(k_pages, "k_pages")
+    cache, _, _, heads = _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, None)
+    _need(heads == hkv, "k and the pages disagree on the number of heads")
+    h, ldq, qt, qp, qo = 1, 0, 0, 0, 0
     if q is not None:
         tq, h, dq, ldq = _rows(q, "q")
         _need(tq == t and dq == hd, "q and k disagree on T or head_dim")
-        qt = _dtype(q)
+        qt = _type_of(q, names)
         if q_out is None:
-            q_out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
-        _need(q_out.dtype is q.dtype and q_out.shape == q.shape and q_out.is_contiguous(),
-              "q_out must be like q, contiguous")
+            q_out = names.empty((t, h, hd), dtype=q.dtype, device=q.device)
+        else:
+            _like(q_out, q, q.dtype, "q_out")
+        qp, qo = q.data_ptr(), q_out.data_ptr()
     else:
         q_out = None
+    at = 0
     if positions is not None:
-        _int32(positions, (t,), "positions")
-    _same_device(k, q, v, k_pages, v_pages, page_table, cache_pos, tok_start, positions, freqs, q_weight, k_weight, q_out)
-    cache = _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, None)
-    rot = _rotation(freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
-    _check(lib().sirius_kv_append(_ptr(q), qt, ldq, _ptr(k), _ptr(v), _dtype(k), ldk, ldv, ctypes.byref(cache),
-                                  _ptr(positions), h, ctypes.byref(rot), _ptr(q_out), _handle()))
+        _vector(positions, names.i32, t, "positions")
+        at = positions.data_ptr()
+    rot = _rotation(names, freqs, interleaved, mscale, norm_eps, q_weight, k_weight, hd)
+    rc = (_lib or lib()).sirius_kv_append(qp, qt, ldq, k.data_ptr(), v.data_ptr(), _type_of(k, names), ldk, ldv, cache, at, h, rot, qo,
+                                          _handle())
+    if rc:
+        _check(rc)
     return q_out
 
 
@@ -707,38 +751,47 @@ def sirius_attn_paged(q, k_pages, v_pages, page_table, cache_pos, *, tok_start=N
     bits. Returns out [T, H, hd] of q's type."""
     if stream is not None:
         return _on(stream, sirius_attn_paged, locals())
-    if _elsewhere(q):
-        return _there(q, sirius_attn_paged, locals())
-    torch = _torch()
+    names = _names or _bound()
+    dev = q.get_device()
+    if dev >= 0 and dev != names.current():
+        args = dict(locals())
+        del args["names"], args["dev"]
+        return _there(q, sirius_attn_paged, args)
+    _on_gpu(dev, k_pages, v_pages, page_table, cache_pos, tok_start, slopes, mask, out, ws)
     t, h, hd, ldq = _rows(q, "q")
-    qt = _dtype(q)
+    qt = _type_of(q, names)
     if out is None:
-        out = torch.empty((t, h, hd), dtype=q.dtype, device=q.device)
-    _need(out.dtype is q.dtype and out.shape == q.shape and out.is_contiguous(), "out must be like q, contiguous")
+        out = names.empty((t, h, hd), dtype=q.dtype, device=q.device)
+    else:
+        _like(out, q, q.dtype, "out")
+    sl = bits = 0
     if slopes is not None:
-        _need(slopes.dtype is torch.float32 and tuple(slopes.shape) == (h,) and slopes.is_contiguous(),
-              "slopes must be fp32 [H], contiguous")
+        _vector(slopes, names.f32, h, "slopes")
+        sl = slopes.data_ptr()
     if mask is not None:
-        _need(mask.dtype is torch.int64 and tuple(mask.shape) == (t,) and mask.is_contiguous(),
-              "mask must be int64 [T], contiguous")
-    _same_device(q, k_pages, v_pages, page_table, cache_pos, tok_start, slopes, mask, out, ws)
-    cache = _paged(t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n)
+        _vector(mask, names.i64, t, "mask")
+        bits = mask.data_ptr()
+    _four(k_pages, "k_pages")
+    cache, bsz, n, hkv = _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n)
     if ws is None:
-        ws = workspace(OP_ATTN_PAGED, cache.B, cache.max_n, h * 65536 + cache.n_kv_heads, hd, device=q.device)
-    _check(lib().sirius_attn_paged(_ptr(q), qt, ldq, ctypes.byref(cache), h, scale, softcap, _ptr(slopes), window,
-                                   _ptr(mask), _ptr(out), _ptr(ws), ws.numel(), _handle()))
+        ws = workspace(OP_ATTN_PAGED, bsz, n, h * 65536 + hkv, hd, device=q.device)
+    rc = (_lib or lib()).sirius_attn_paged(q.data_ptr(), qt, ldq, cache, h, scale, softcap, sl, window, bits, out.data_ptr(),
+                                           ws.data_ptr(), ws.numel(), _handle())
+    if rc:
+        _check(rc)
     return out
 
 
 def _per_row(v, dtype, bsz, device, name):
-    """A parameter of sampling: None, a [B] tensor, or one value for every row."""
-    torch = _torch()
+    """The address of a parameter of sampling (None: 0, a [B] tensor, or one value for every row), and what keeps it."""
     if v is None:
-        return None
+        return 0, None
+    torch = _torch()
     if not isinstance(v, torch.Tensor):
-        return torch.full((bsz,), v, dtype=dtype, device=device)
-    _need(v.dtype is dtype and tuple(v.shape) == (bsz,) and v.is_contiguous(), f"{name} must be {dtype} [B], contiguous")
-    return v
+        v = torch.full((bsz,), v, dtype=dtype, device=device)
+    else:
+        _vector(v, dtype, bsz, name)
+    return v.data_ptr(), v
 
 
 def sirius_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, token=None, kept=None, prob=None,
@@ -748,34 +801,40 @@ def sirius_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
     [B] int32, prob [B] fp32)."""
     if stream is not None:
         return _on(stream, sirius_sample, locals())
-    if _elsewhere(logits):
-        return _there(logits, sirius_sample, locals())
-    torch = _torch()
-    _need(logits.dtype is torch.float32 and logits.dim() == 2, "logits must be fp32 [B, V]")
-    _need(logits.is_cuda, "tensors must live on the GPU")
+    names = _names or _bound()
+    dev = logits.get_device()
+    if dev >= 0 and dev != names.current():
+        args = dict(locals())
+        del args["names"], args["dev"]
+        return _there(logits, sirius_sample, args)
+    f32, i32 = names.f32, names.i32
+    _need(logits.dtype is f32 and logits.dim() == 2, "logits must be fp32 [B, V]")
+    _on_gpu(dev, u, token, kept, prob, ws, *(v for v in (temperature, top_k, top_p, min_p) if hasattr(v, "get_device")))
     bsz, vocab = logits.shape
-    _need(bsz == 0 or vocab <= 1 or logits.stride(1) == 1, "a row's logits must be contiguous")
-    ld = logits.stride(0) if bsz > 1 else vocab
-    dev = logits.device
-    f32, i32 = torch.float32, torch.int32
-    _need(u.dtype is f32 and tuple(u.shape) == (bsz,) and u.is_contiguous(), "u must be fp32 [B], contiguous")
-    temperature = _per_row(temperature, f32, bsz, dev, "temperature")
-    top_k, top_p = _per_row(top_k, i32, bsz, dev, "top_k"), _per_row(top_p, f32, bsz, dev, "top_p")
-    min_p = _per_row(min_p, f32, bsz, dev, "min_p")
-    if token is None:
-        token = torch.empty(bsz, dtype=i32, device=dev)
-    if kept is None:
-        kept = torch.empty(bsz, dtype=i32, device=dev)
-    if prob is None:
-        prob = torch.empty(bsz, dtype=f32, device=dev)
-    for t, d, n in ((token, i32, "token"), (kept, i32, "kept"), (prob, f32, "prob")):
-        _need(t.dtype is d and tuple(t.shape) == (bsz,) and t.is_contiguous(), f"{n} must be {d} [B], contiguous")
-    _same_device(logits, u, temperature, top_k, top_p, min_p, token, kept, prob, ws)
+    ld = vocab
+    if bsz > 0 and not logits.is_contiguous():
+        _need(vocab <= 1 or logits.stride(1) == 1, "a row's logits must be contiguous")
+        ld = logits.stride(0) if bsz > 1 else vocab
+    where = logits.device
+    _vector(u, f32, bsz, "u")
+    t, hold_t = _per_row(temperature, f32, bsz, where, "temperature")
+    k, hold_k = _per_row(top_k, i32, bsz, where, "top_k")
+    p, hold_p = _per_row(top_p, f32, bsz, where, "top_p")
+    m, hold_m = _per_row(min_p, f32, bsz, where, "min_p")
+    outs = []
+    for o, d, name in ((token, i32, "token"), (kept, i32, "kept"), (prob, f32, "prob")):
+        if o is None:
+            o = names.empty(bsz, dtype=d, device=where)
+        else:
+            _vector(o, d, bsz, name)
+        outs.append(o)
     if ws is None:
-        ws = workspace(OP_SAMPLE, bsz, 0, 0, vocab, device=dev)
-    _check(lib().sirius_sample(_ptr(logits), ld, bsz, vocab, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
-                               _ptr(token), _ptr(kept), _ptr(prob), _ptr(ws), ws.numel(), _handle()))
-    return token, kept, prob
+        ws = workspace(OP_SAMPLE, bsz, 0, 0, vocab, device=where)
+    rc = (_lib or lib()).sirius_sample(logits.data_ptr(), ld, bsz, vocab, u.data_ptr(), t, k, p, m, outs[0].data_ptr(),
+                                       outs[1].data_ptr(), outs[2].data_ptr(), ws.data_ptr(), ws.numel(), _handle())
+    if rc:
+        _check(rc)
+    return tuple(outs)
 
 
 def sirius_rmsnorm(h, eps=1e-5, *, out=None, stream=None):

@@ -113,8 +113,14 @@ __device__ __forceinline__ int wave_add(int v) {
   return v;
 }
 
-// The unit with this number, b = -1 behind the last. Every workgroup counts for itself: one sequence
-// per thread, the total of the visible rows first, then the units before.
+__device__ __forceinline__ int rows_per_unit(const Args& a, long total) {
+  const int length = (int)max((total + a.units - 1) / a.units, 1l);
+  return (length + kStep - 1) / kStep * kStep;
+}
+
+// The unit with this number, b = -1 behind the last. Every workgroup counts for itself, one sequence
+// per lane: the total of the visible rows first, then the units before. Up to 64 sequences every wave
+// does so alone; more take the whole workgroup, 256 at a time.
 __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
   __shared__ int s_w[2][kWaves];
   __shared__ int s_hit[5];
@@ -122,9 +128,39 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
   const int B = a.pg.B;
   Unit u{};
   int length = 1 << 30;  // rows per unit
+  // inclusive sums of a sequence's units and of its partial slots over the wave
+  auto scan = [&](int& ic, int& is) {
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int c = __shfl_up(ic, o, kWave), d = __shfl_up(is, o, kWave);
+      if (lane >= o) {
+        ic += c;
+        is += d;
+      }
+    }
+  };
+  auto cut = [&](int span, int count) {  // equal units of whole steps
+    const int l = (span + count - 1) / count;
+    return (l + kStep - 1) / kStep * kStep;
+  };
   if (a.units <= 1) {
     u.b = number < B ? number : -1;
     u.count = 1;
+  } else if (B <= kWave) {
+    const int s = lane < B ? span_of(a, lane) : 0;
+    const int every = rows_per_unit(a, wave_add(s));
+    const int cnt = (s + every - 1) / every, sl = cnt > 1 ? cnt : 0;
+    int ic = cnt, is = sl;
+    scan(ic, is);
+    const uint64_t hit = __ballot(number >= ic - cnt && number < ic);
+    if (hit == 0) {
+      u.b = -1;
+      return u;
+    }
+    u.b = __builtin_ctzll(hit);
+    u.count = __shfl(cnt, u.b, kWave);
+    u.slot = __shfl(is - sl, u.b, kWave);
+    u.part = number - __shfl(ic - cnt, u.b, kWave);
+    length = cut(__shfl(s, u.b, kWave), u.count);
   } else {
     long total = 0;
     for (int b0 = 0; b0 < B; b0 += kThreads) {
@@ -135,21 +171,14 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
       total += (long)s_w[0][0] + s_w[0][1] + s_w[0][2] + s_w[0][3];
       __syncthreads();
     }
-    length = (int)max((total + a.units - 1) / a.units, 1l);
-    length = (length + kStep - 1) / kStep * kStep;
+    const int every = rows_per_unit(a, total);
     int before = 0, slots = 0;  // units and partial slots before this block
     if (tid == 0) s_hit[0] = -1;
     for (int b0 = 0; b0 < B; b0 += kThreads) {
       const int s = b0 + tid < B ? span_of(a, b0 + tid) : 0;
-      const int cnt = (s + length - 1) / length, sl = cnt > 1 ? cnt : 0;
+      const int cnt = (s + every - 1) / every, sl = cnt > 1 ? cnt : 0;
       int ic = cnt, is = sl;
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int c = __shfl_up(ic, o, kWave), d = __shfl_up(is, o, kWave);
-        if (lane >= o) {
-          ic += c;
-          is += d;
-        }
-      }
+      scan(ic, is);
       if (lane == kWave - 1) {
         s_w[0][wave] = ic;
         s_w[1][wave] = is;
@@ -174,11 +203,16 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
     }
     u.b = s_hit[0];
     if (u.b < 0) return u;
+    u.part = s_hit[1];
     u.count = s_hit[2];
     u.slot = s_hit[3];
-    length = (s_hit[4] + u.count - 1) / u.count;
-    length = (length + kStep - 1) / kStep * kStep;
+    length = cut(s_hit[4], u.count);
   }
+  u.b = __builtin_amdgcn_readfirstlane(u.b);
+  u.part = __builtin_amdgcn_readfirstlane(u.part);
+  u.count = __builtin_amdgcn_readfirstlane(u.count);
+  u.slot = __builtin_amdgcn_readfirstlane(u.slot);
+  length = __builtin_amdgcn_readfirstlane(length);
   if (u.b < 0) return u;
   const int2 tk = tokens_of(a.pg, u.b);
   u.first = tk.x;
@@ -191,7 +225,6 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
   }
   if (!valid(a, u.p, u.n)) return u;  // c0 = c1
   const int base = u.lo & ~(kTile - 1);
-  u.part = a.units <= 1 ? 0 : s_hit[1];
   u.c0 = (int)min((long)base + (long)u.part * length, (long)u.p + u.n);
   u.c1 = (int)min((long)u.c0 + length, (long)u.p + u.n);
   return u;

@@ -21,15 +21,33 @@ def lib():
     return _lib
 
 
+class RotationC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("freqs", "q_weight", "k_weight")] + \
+               [("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int), ("mscale", ctypes.c_float), ("norm_eps", ctypes.c_float)]
+
+
+class PagedC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "cache_pos", "tok_start")] + \
+               [(n, ctypes.c_int) for n in ("B", "T", "max_n", "n_kv_heads", "head_dim", "n_pages", "page_size", "max_pages")]
+
+
+def test_the_binding_packs_the_structs(lib):
+    assert lib._ROTATION.size == ctypes.sizeof(RotationC) and lib._PAGED.size == ctypes.sizeof(PagedC)
+    r = RotationC.from_buffer_copy(lib._ROTATION.pack(8, 16, 24, 64, 1, 1.5, -1.0))
+    assert (r.freqs, r.q_weight, r.k_weight, r.rot_dim, r.interleaved, r.mscale, r.norm_eps) == (8, 16, 24, 64, 1, 1.5, -1.0)
+    c = PagedC.from_buffer_copy(lib._PAGED.pack(*range(1, 14)))
+    assert [getattr(c, n) for n, _ in PagedC._fields_] == list(range(1, 14))
+
+
 def _rotation(lib, **kw):
     r = dict(freqs=1 << 20, q_weight=None, k_weight=None, rot_dim=64, interleaved=0, mscale=1.0, norm_eps=-1.0)
-    return lib._RotationC(*(r | kw).values())
+    return RotationC(*(r | kw).values())
 
 
 def _paged(lib, **kw):
     c = dict(k_pages=1 << 20, v_pages=1 << 21, page_table=1 << 20, cache_pos=1 << 20, tok_start=None, B=2, T=6, max_n=3,
              n_kv_heads=2, head_dim=64, n_pages=9, page_size=16, max_pages=4)
-    return lib._PagedC(*(c | kw).values())
+    return PagedC(*(c | kw).values())
 
 
 BAD_ROTATIONS = [dict(rot_dim=7), dict(rot_dim=66), dict(rot_dim=-2), dict(freqs=None), dict(mscale=NAN), dict(mscale=INF),
@@ -90,7 +108,7 @@ def test_binding_refusals(lib):
         lib.sirius_rope(x, x, pos, f)
     with pytest.raises(ValueError):
         lib.sirius_rope(None, None, pos, f)
-    with pytest.raises(ValueError, match="heads, head_dim"):
+    with pytest.raises(ValueError):
         lib.sirius_rope(x[0], None, pos, f)
     pages, table = torch.zeros(2, 4, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 2, dtype=torch.int32)
     with pytest.raises(ValueError):
