@@ -10,7 +10,7 @@
 // batches stay balanced. A sequence of one unit is written out directly; the others leave (max, sum,
 // output) per unit and row, and attn_paged_merge_kernel joins them in order.
 //
-// attn_rows_kernel: up to 16 QT query rows per workgroup, four waves that take every fourth tile of
+// attn_rows_kernel: up to 16 query rows per workgroup, four waves that take every fourth tile of
 // 32 positions each and are merged at the end. Scores are K Q^T on the matrix units, whose result (a lane
 // holds one query row and, by the order in which key rows are dealt to the operand's rows, eight
 // consecutive positions) is the operand of V^T P^T as it is. Keys lie row by row and values column by
@@ -246,8 +246,11 @@ __device__ __forceinline__ float value_at(const uint16_t* p, int i) { return bf1
 struct RowLimits {
   int low, last, p;  // rows low .. last, of those from p on the ones whose bit is set
   uint64_t bits;
+  // Without branches: five instructions a position (and with short circuits this compiler has lost the
+  // assignment that hides a position)
   __device__ __forceinline__ bool sees(int pos) const {
-    return pos >= low && pos <= last && (pos < p || ((bits >> (pos - p)) & 1) != 0);
+    const int k = pos - p;
+    return (pos >= low) & (pos <= last) & ((k < 0) | (((bits >> (k & 63)) & 1) != 0));
   }
 };
 template <bool MOD>
@@ -413,11 +416,12 @@ __device__ __forceinline__ void modify(const Args& a, float* x, const RowLimits&
 // KS: 32-wide steps of the head size. MOD: any of cap, slopes, window, mask.
 template <typename TQ, int KS, bool MOD>
 __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
-  constexpr int QT = 1;
   constexpr bool kF32 = sizeof(TQ) == 4;
   constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : 2;  // pieces of queries and probabilities
   constexpr int kHd = KS * 32, DT = KS * 2;
   __shared__ uint2 s_page[kGroups];  // page, offset of an 8-position group
+  // the queries' pieces stay in LDS: they would take 48 of the 256 registers
+  __shared__ uint4 s_q[kF32 ? KS * NQ * kWave : 1];
   __shared__ int s_bad, s_nan;
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][kHd + 4];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
   const int kvh = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv % a.rgroups;
   const Unit u = find_unit(a, blockIdx.x / (a.Hkv * a.rgroups));
   if (u.b < 0) return;
-  const int R = a.G * a.pg.n, r0 = rg * 16 * QT, nrows = u.n * a.G;
+  const int R = a.G * a.pg.n, r0 = rg * 16, nrows = u.n * a.G;
   if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
   if (u.c1 <= u.c0 && !valid(a, u.p, u.n)) {
     // every row, also those behind the row groups that the call was launched for
@@ -435,33 +439,31 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
     return;
   }
   if (r0 >= nrows) return;
-  const int nr = min(16 * QT, nrows - r0);
+  const int nr = min(16, nrows - r0);
   const size_t prow = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R + r0;  // this unit's partial rows
   // positions that the group's rows see at all
   const int last = u.p + (r0 + nr - 1) / a.G;
   const int c1 = min(u.c1, last + 1);
   // ---- queries: the B operand, lane (row, 8 columns of each step)
-  bf16x8_t qf[QT][KS][NQ];
-  RowLimits lim[QT];
-  float slope[QT];
+  bf16x8_t qf[KS][NQ];
+  const int row = r0 + fr, qi = row / a.G, qh = kvh * a.G + (row - qi * a.G);
+  const bool there = row < nrows;
+  const RowLimits lim = limits<MOD>(a, u, row, nrows);
+  const float slope = MOD && a.slopes != nullptr && there ? a.slopes[qh] : 0.f;
+  if (!kF32 || wave == 0) {
+    load_query<TQ, KS, NQ>(static_cast<const TQ*>(a.q) + (long)(u.first + (there ? qi : 0)) * a.ldq + (long)(there ? qh : 0) * a.hd,
+                           there, g, hd8, qf);
+    if constexpr (kF32) {
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = r0 + 16 * t + fr, i = r / a.G, h = kvh * a.G + (r - i * a.G);
-    const bool there = r < nrows;
-    lim[t] = limits<MOD>(a, u, r, nrows);
-    slope[t] = MOD && a.slopes != nullptr && there ? a.slopes[h] : 0.f;
-    load_query<TQ, KS, NQ>(static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd,
-                           there, g, hd8, qf[t]);
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int pc = 0; pc < NQ; ++pc) s_q[(s * NQ + pc) * kWave + lane] = __builtin_bit_cast(uint4, qf[s][pc]);
+    }
   }
-  float m[QT], l[QT];
-  floatx4_t o[QT][DT];  // columns 16 d + 4 g + e of row fr
+  float m = -FLT_MAX, l = 0.f;
+  floatx4_t o[DT];  // columns 16 d + 4 g + e of row fr
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -FLT_MAX;
-    l[t] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[t][d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < DT; ++d) o[d] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
   const int low_last = MOD && a.window > 0 ? max(0, last + 1 - a.window) : 0;  // below it some row sees nothing
   const float slack = kF32 || MOD ? 4.f : 4.f / a.scale;
@@ -486,7 +488,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
     for (int d = 0; d < DT; ++d)
       f.v[d] = 16 * d + fr < a.hd ? vp[(size_t)16 * d * (ps >> 3)] : make_uint4(0u, 0u, 0u, 0u);
   };
+  auto query = [&](int s, int pc) {
+    if constexpr (kF32) return __builtin_bit_cast(bf16x8_t, s_q[(s * NQ + pc) * kWave + lane]);
+    else return qf[s][pc];
+  };
   auto compute = [&](Frag& f, int t0) {
+    if (kF32) asm volatile("" ::: "memory");  // the queries are read again for each tile, not held
     if (t0 + kTile > c1) {  // uniform: nothing of the rows behind reaches the sums
       uint32_t keep[4];
 #pragma unroll
@@ -498,8 +505,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
       for (int d = 0; d < DT; ++d)
         f.v[d] = make_uint4(f.v[d].x & keep[0], f.v[d].y & keep[1], f.v[d].z & keep[2], f.v[d].w & keep[3]);
     }
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
+    {
       float x[8];  // positions t0 + 8 g + e
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -508,20 +514,20 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
         for (int s = 0; s < KS; ++s) {
           const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, f.k[h][s]);
 #pragma unroll
-          for (int pc = NQ - 1; pc > 0; --pc) low = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][pc], low, 0, 0, 0);
-          hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][0], hi, 0, 0, 0);
+          for (int pc = NQ - 1; pc > 0; --pc) low = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, query(s, pc), low, 0, 0, 0);
+          hi = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, query(s, 0), hi, 0, 0, 0);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[4 * h + e] = kF32 ? hi[e] + low[e] : hi[e];
       }
-      modify<MOD, kF32, 8>(a, x, lim[t], slope[t], inv_cap, t0, g);
+      modify<MOD, kF32, 8>(a, x, lim, slope, inv_cap, t0, g);
       // uniform: some row does not see all of it (a mask may hide row p from its own token)
       if (t0 + kTile > min(c1, MOD ? u.p : u.p + 1) || (MOD && t0 < low_last)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int pos = t0 + 8 * g + e;
-          const bool seen = MOD ? lim[t].sees(pos) : pos <= lim[t].last;
-          if (!seen || pos >= c1) x[e] = -INFINITY;
+          const bool seen = MOD ? lim.sees(pos) : pos <= lim.last;
+          x[e] = (seen & (pos < c1)) ? x[e] : -INFINITY;
         }
       }
       float mx = x[0];
@@ -529,30 +535,30 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
       for (int e = 1; e < 8; ++e) mx = __builtin_elementwise_maximum(mx, x[e]);
       const float c = MOD ? 1.44269504088896341f : to_exp2;
       // sums stay on their maximum until some score is e^4 above it (or a NaN)
-      if (__ballot(!(mx <= m[t] + slack)) != 0) {
+      if (__ballot(!(mx <= m + slack)) != 0) {
         mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 16, kWave));
         mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, kWave));
-        const float m_new = __builtin_elementwise_maximum(m[t], mx);
-        const float alpha = kF32 ? exp_neg(m[t] - m_new) : __builtin_amdgcn_exp2f((m[t] - m_new) * c);
-        m[t] = m_new;
-        l[t] *= alpha;
+        const float m_new = __builtin_elementwise_maximum(m, mx);
+        const float alpha = kF32 ? exp_neg(m - m_new) : __builtin_amdgcn_exp2f((m - m_new) * c);
+        m = m_new;
+        l *= alpha;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+        for (int d = 0; d < DT; ++d) o[d] *= alpha;
       }
       float pr[8], sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        pr[e] = kF32 ? exp_neg(x[e] - m[t]) : __builtin_amdgcn_exp2f((x[e] - m[t]) * c);
+        pr[e] = kF32 ? exp_neg(x[e] - m) : __builtin_amdgcn_exp2f((x[e] - m) * c);
         sum += pr[e];
       }
-      l[t] += sum;
+      l += sum;
       bf16x8_t pf[NP];
       pieces<NP>(pr, pf);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int pc = NP - 1; pc >= 0; --pc)
-          o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f.v[d]), pf[pc], o[t][d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f.v[d]), pf[pc], o[d], 0, 0, 0);
     }
   };
   for (int seg = u.c0; seg < c1; seg += kGroups * 8) {
@@ -581,13 +587,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
     }
   }
   // ---- the waves' shares joined in order, one query tile at a time
+  {
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    floatx4_t chk = floatx4_t{l, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    l[t] += __shfl_xor(l[t], 16, kWave);
-    l[t] += __shfl_xor(l[t], 32, kWave);
-    floatx4_t chk = floatx4_t{l[t], 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int d = 0; d < DT; ++d) chk += o[t][d];
+    for (int d = 0; d < DT; ++d) chk += o[d];
     const float c = (chk[0] + chk[1]) + (chk[2] + chk[3]);
     // infinite sums count: they may be an overflow's, or an infinite value's, which the pieces turned
     if (__ballot(!(fabsf(c) < INFINITY)) != 0 && lane == 0) s_nan = 1;
@@ -604,25 +609,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
       whole_row<TQ>(a, w, r0 + r, kvh, u.count > 1 ? a.po + (prow + r) * a.hd : nullptr, a.pm + prow + r, a.pl + prow + r);
     return;
   }
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    if (t > 0) __syncthreads();
+  {
     if (g == 0) {
-      s_m[wave][fr] = l[t] > 0.f ? m[t] : -INFINITY;
-      s_l[wave][fr] = l[t];
+      s_m[wave][fr] = l > 0.f ? m : -INFINITY;
+      s_l[wave][fr] = l;
     }
     __syncthreads();
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][fr]);
     const float unit = kF32 || MOD ? 1.f : a.scale;  // m counts unscaled scores there
-    const float f = l[t] > 0.f ? expf((m[t] - M) * unit) : 0.f;
+    const float f = l > 0.f ? expf((m - M) * unit) : 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
       *reinterpret_cast<float4*>(&s_o[wave][fr][16 * d + 4 * g]) =
-          make_float4(o[t][d][0] * f, o[t][d][1] * f, o[t][d][2] * f, o[t][d][3] * f);
+          make_float4(o[d][0] * f, o[d][1] * f, o[d][2] * f, o[d][3] * f);
     __syncthreads();
-    const int rows = min(16, nr - 16 * t);
+    const int rows = nr;
     for (int e = tid; e < rows * (kHd / 4); e += kThreads) {
       const int rr = e / (kHd / 4), c = 4 * (e % (kHd / 4));
       if (c >= a.hd) continue;
@@ -637,9 +640,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
         const float mw = s_m[w][rr];
         lt += mw > -INFINITY ? s_l[w][rr] * expf((mw - Mr) * unit) : 0.f;
       }
-      const int r = r0 + 16 * t + rr;
+      const int r = r0 + rr;
       if (u.count > 1) {
-        const size_t row = prow + 16 * t + rr;
+        const size_t row = prow + rr;
         *reinterpret_cast<float4*>(a.po + row * a.hd + c) = v;
         if (c == 0) {
           a.pm[row] = Mr * (Mr > -INFINITY ? unit : 1.f);
@@ -830,7 +833,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
           for (int e = 0; e < 8; ++e) {
             const int pos = t0 + 32 * nb + 8 * g + e;
             const bool seen = MOD ? lim[t].sees(pos) : pos <= lim[t].last;
-            if (!seen || pos >= c1) x[t][nb][e] = -INFINITY;
+            x[t][nb][e] = (seen & (pos < c1)) ? x[t][nb][e] : -INFINITY;
           }
       }
       float mx = x[t][0][0];
@@ -1001,9 +1004,10 @@ __global__ __launch_bounds__(kThreads) void attn_paged_merge_kernel(Args a) {
   }
 }
 
-// Query rows of a workgroup: up to 32 rows by the sixteen on the kernel without LDS, more by 64, and
-// bf16 ones by 128 where there are that many.
-constexpr int kFewRows = 32;
+// Query rows of a workgroup: up to 16 on the kernel without LDS, more by 64, and bf16 ones by 128 where
+// there are more than 64. (24 bf16 rows over 48 sequences of up to 30000 rows: 300 us in tiles, 426 as twice
+// 16 rows; 12 rows 305 us there.)
+constexpr int kFewRows = 16;
 int group_rows(int rows, bool bf16) { return rows <= kFewRows ? 16 : !bf16 || rows <= 64 ? 64 : 128; }
 
 }  // namespace
