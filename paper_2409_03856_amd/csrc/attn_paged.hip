@@ -40,14 +40,14 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;           // positions per wave step
 constexpr int kStep = kTile * kWaves;
 constexpr int kTargetWgs = 512;     // workgroups wanted: two per CU
-constexpr int kMaxUnits = 256;      // ranges that the whole call is cut into at most, besides whole sequences
+constexpr int kMaxUnits = 256;      // units of a round at most
 constexpr int kGroups = 512;        // 8-position groups whose pages are staged at a time
 
 struct Args {
   PagedView pg;
   const void* q;
   long ldq;
-  int H, Hkv, hd, G, rgroups, units;  // units: ranges wanted (1: every sequence whole)
+  int H, Hkv, hd, G, rgroups, units, rounds;  // units: ranges of a round (1: every sequence whole); rounds: 1 or 2
   float scale, cap;
   const float* slopes;
   int window;
@@ -113,72 +113,104 @@ __device__ __forceinline__ int wave_add(int v) {
   return v;
 }
 
-__device__ __forceinline__ int rows_per_unit(const Args& a, long total) {
-  const int length = (int)max((total + a.units - 1) / a.units, 1l);
-  return (length + kStep - 1) / kStep * kStep;
+__device__ __forceinline__ int whole_steps(long rows) { return (int)((max(rows, 1l) + kStep - 1) / kStep * kStep); }
+
+// How the call's sequences are cut. Every workgroup counts for itself, one sequence per lane.
+struct Plan {
+  int every;          // rows per unit at most
+  int span, cnt;      // up to 64 sequences: this lane's
+  int ic, is;         // and the units and the partial slots up to its end
+};
+
+// Inclusive sums over the wave.
+__device__ __forceinline__ void scan2(int lane, int& a, int& b) {
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int c = __shfl_up(a, o, kWave), d = __shfl_up(b, o, kWave);
+    if (lane >= o) {
+      a += c;
+      b += d;
+    }
+  }
 }
 
-// The unit with this number, b = -1 behind the last. Every workgroup counts for itself, one sequence
-// per lane: the total of the visible rows first, then the units before. Up to 64 sequences every wave
-// does so alone; more take the whole workgroup, 256 at a time.
-__device__ __forceinline__ Unit find_unit(const Args& a, int number) {
+// Up to 64 sequences every wave plans alone; more take the whole workgroup, 256 at a time.
+__device__ __forceinline__ Plan make_plan(const Args& a) {
+  constexpr int kOvh = 256;  // what a unit costs besides its rows, in rows
+  __shared__ int s_w[kWaves];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, B = a.pg.B;
+  Plan p{1 << 30, 0, 0, 0, 0};
+  if (a.units <= 1) return p;
+  if (B > kWave) {
+    long total = 0;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+      // spans are at most 2^20: a block's sum fits an int
+      const int s = wave_add(b0 + tid < B ? span_of(a, b0 + tid) : 0);
+      if (lane == 0) s_w[wave] = s;
+      __syncthreads();
+      total += (long)s_w[0] + s_w[1] + s_w[2] + s_w[3];
+      __syncthreads();
+    }
+    p.every = whole_steps((total + a.units * a.rounds - 1) / (a.units * a.rounds));
+    return p;
+  }
+  p.span = lane < B ? span_of(a, lane) : 0;
+  const int total = wave_add(p.span);
+  p.every = whole_steps((total + a.units - 1) / a.units);
+  if (a.rounds > 1 && B > 1) {
+    // One or two rounds of a.units units of equal length, or as many units for every sequence as one
+    // round has room for: what ends first. 8 sequences of 6000 rows in 21 units go by two each, not by three
+    // in 24 (213 -> 181 us).
+    int most = p.span;
+    for (int m = 1; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m, kWave));
+    const int half = whole_steps((total + 2 * a.units - 1) / (2 * a.units));
+    const int one = wave_add((p.span + p.every - 1) / p.every), two = wave_add((p.span + half - 1) / half);
+    auto cost = [&](int units, int rows) { return (units + a.units - 1) / a.units * (rows + kOvh); };
+    int best = cost(one, p.every);
+    if (cost(two, half) < best) {
+      best = cost(two, half);
+      p.every = half;
+    }
+    const int fit = B <= a.units ? whole_steps((most + a.units / B - 1) / (a.units / B)) : INT32_MAX / 2;
+    if (fit + kOvh < best) p.every = fit;
+  }
+  p.cnt = (p.span + p.every - 1) / p.every;
+  p.ic = p.cnt;
+  p.is = p.cnt > 1 ? p.cnt : 0;
+  scan2(lane, p.ic, p.is);
+  return p;
+}
+
+// The unit with this number, b = -1 behind the last.
+__device__ __forceinline__ Unit unit_at(const Args& a, const Plan& p, int number) {
   __shared__ int s_w[2][kWaves];
   __shared__ int s_hit[5];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
   const int B = a.pg.B;
   Unit u{};
   int length = 1 << 30;  // rows per unit
-  // inclusive sums of a sequence's units and of its partial slots over the wave
-  auto scan = [&](int& ic, int& is) {
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int c = __shfl_up(ic, o, kWave), d = __shfl_up(is, o, kWave);
-      if (lane >= o) {
-        ic += c;
-        is += d;
-      }
-    }
-  };
-  auto cut = [&](int span, int count) {  // equal units of whole steps
-    const int l = (span + count - 1) / count;
-    return (l + kStep - 1) / kStep * kStep;
-  };
+  auto cut = [&](int span, int count) { return whole_steps((span + count - 1) / count); };
   if (a.units <= 1) {
     u.b = number < B ? number : -1;
     u.count = 1;
   } else if (B <= kWave) {
-    const int s = lane < B ? span_of(a, lane) : 0;
-    const int every = rows_per_unit(a, wave_add(s));
-    const int cnt = (s + every - 1) / every, sl = cnt > 1 ? cnt : 0;
-    int ic = cnt, is = sl;
-    scan(ic, is);
-    const uint64_t hit = __ballot(number >= ic - cnt && number < ic);
+    const uint64_t hit = __ballot(number >= p.ic - p.cnt && number < p.ic);
     if (hit == 0) {
       u.b = -1;
       return u;
     }
     u.b = __builtin_ctzll(hit);
-    u.count = __shfl(cnt, u.b, kWave);
-    u.slot = __shfl(is - sl, u.b, kWave);
-    u.part = number - __shfl(ic - cnt, u.b, kWave);
-    length = cut(__shfl(s, u.b, kWave), u.count);
+    u.count = __shfl(p.cnt, u.b, kWave);
+    u.slot = __shfl(p.is, u.b, kWave) - (u.count > 1 ? u.count : 0);
+    u.part = number - (__shfl(p.ic, u.b, kWave) - u.count);
+    length = cut(__shfl(p.span, u.b, kWave), u.count);
   } else {
-    long total = 0;
-    for (int b0 = 0; b0 < B; b0 += kThreads) {
-      // spans are at most 2^20: a block's sum fits an int
-      const int s = wave_add(b0 + tid < B ? span_of(a, b0 + tid) : 0);
-      if (lane == 0) s_w[0][wave] = s;
-      __syncthreads();
-      total += (long)s_w[0][0] + s_w[0][1] + s_w[0][2] + s_w[0][3];
-      __syncthreads();
-    }
-    const int every = rows_per_unit(a, total);
     int before = 0, slots = 0;  // units and partial slots before this block
     if (tid == 0) s_hit[0] = -1;
     for (int b0 = 0; b0 < B; b0 += kThreads) {
       const int s = b0 + tid < B ? span_of(a, b0 + tid) : 0;
-      const int cnt = (s + every - 1) / every, sl = cnt > 1 ? cnt : 0;
+      const int cnt = (s + p.every - 1) / p.every, sl = cnt > 1 ? cnt : 0;
       int ic = cnt, is = sl;
-      scan(ic, is);
+      scan2(lane, ic, is);
       if (lane == kWave - 1) {
         s_w[0][wave] = ic;
         s_w[1][wave] = is;
@@ -219,11 +251,7 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int number) {
   u.n = tk.y;
   u.p = a.pg.pos[u.b];
   u.lo = first_seen(a, u.p);
-  if (u.n == 0 && a.units <= 1) {
-    u.b = -1;
-    return u;
-  }
-  if (!valid(a, u.p, u.n)) return u;  // c0 = c1
+  if (u.n == 0 || !valid(a, u.p, u.n)) return u;  // c0 = c1
   const int base = u.lo & ~(kTile - 1);
   u.c0 = (int)min((long)base + (long)u.part * length, (long)u.p + u.n);
   u.c1 = (int)min((long)u.c0 + length, (long)u.p + u.n);
@@ -429,7 +457,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
   const int fr = lane & 15, g = lane >> 4, hd8 = a.hd >> 3, ps = a.pg.page_size;
   // heads fastest: workgroups of one head run on one XCD where there are 8 of them
   const int kvh = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv % a.rgroups;
-  const Unit u = find_unit(a, blockIdx.x / (a.Hkv * a.rgroups));
+  const Unit u = unit_at(a, make_plan(a), blockIdx.x / (a.Hkv * a.rgroups));
   if (u.b < 0) return;
   const int R = a.G * a.pg.n, r0 = rg * 16, nrows = u.n * a.G;
   if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
@@ -685,7 +713,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   const int fr = lane & 15, g = lane >> 4, hd8 = a.hd >> 3, ps = a.pg.page_size;
   // the longest rows of a prompt first; heads fastest, so that with 8 of them a head stays on one XCD
   const int kvh = blockIdx.x % a.Hkv, rg = a.rgroups - 1 - blockIdx.x / a.Hkv % a.rgroups;
-  const Unit u = find_unit(a, blockIdx.x / (a.Hkv * a.rgroups));
+  const Unit u = unit_at(a, make_plan(a), blockIdx.x / (a.Hkv * a.rgroups));
   if (u.b < 0) return;
   const int R = a.G * a.pg.n, r0 = rg * 64 * QT, nrows = u.n * a.G;
   if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
@@ -1017,10 +1045,13 @@ PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf1
   const int R = H / Hkv * n;
   L.rgroups = ceil_div(std::max(R, 1), group_rows(R, bf16));
   const long wgs = (long)Hkv * L.rgroups;
-  L.units = (int)std::min<long>((kTargetWgs + wgs - 1) / wgs, kMaxUnits);
-  // A unit is at least the average row count over `units`: sequences of more than one unit make fewer
-  // than 2 units of them.
-  const size_t rows = L.units > 1 ? (size_t)2 * L.units * Hkv * R : 0;
+  // Few rows are bound by memory, which one round and what is over keeps busy; tiles by the matrix units, so
+  // a second round that is not full costs as much as a full one.
+  L.rounds = R <= kFewRows ? 1 : 2;
+  L.units = (int)std::min<long>(std::max((kTargetWgs + (L.rounds == 1 ? wgs - 1 : 0)) / wgs, 1l), kMaxUnits);
+  // A unit is at least the total row count over rounds * units: sequences of more than one unit make fewer
+  // than twice as many of them.
+  const size_t rows = L.units > 1 ? (size_t)2 * L.rounds * L.units * Hkv * R : 0;
   Carve c;
   L.info = c.take((size_t)std::max(B, 1) * sizeof(int2));
   L.pm = c.take(rows * sizeof(float));
@@ -1036,7 +1067,7 @@ hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* 
   a.pg = pg;
   a.q = c.q; a.ldq = c.ldq;
   a.H = c.H; a.Hkv = c.Hkv; a.hd = c.hd; a.G = c.H / c.Hkv;
-  a.rgroups = L.rgroups; a.units = L.units;
+  a.rgroups = L.rgroups; a.units = L.units; a.rounds = L.rounds;
   a.scale = c.scale; a.cap = c.cap; a.slopes = c.slopes; a.window = c.window; a.mask = c.mask;
   a.out = c.out;
   a.info = reinterpret_cast<int2*>(ws + L.info);
@@ -1045,8 +1076,9 @@ hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* 
   a.po = reinterpret_cast<float*>(ws + L.po);
   const bool mod = c.cap > 0.f || c.slopes != nullptr || c.window > 0 || c.mask != nullptr;
   const int R = a.G * pg.n, rows = group_rows(R, c.q_bf16), ks = ceil_div(c.hd, 32);
-  // every sequence has a unit, and the cuts add fewer than `units`
-  const long grid = (long)c.Hkv * L.rgroups * (pg.B + (L.units > 1 ? L.units : 0));
+  // every sequence has a unit, and the cuts add fewer than rounds * units
+  const long most = (long)pg.B * ceil_div(pg.max_pages * pg.page_size + kTile, kStep);
+  const long grid = (long)c.Hkv * L.rgroups * (L.units > 1 ? std::min<long>(pg.B + L.rounds * L.units, most) : pg.B);
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   {
     ProfScope prof("attn_paged", stream);

@@ -249,7 +249,7 @@ hipError_t launch_rope(const RopeCall& c, hipStream_t stream);
 hipError_t launch_kv_append(const RopeCall& c, const PagedView& pg, hipStream_t stream);
 
 struct PagedAttnLayout {
-  int rgroups, units;               // query-row groups per kv head, ranges that the call is cut into
+  int rgroups, units, rounds;       // query-row groups per kv head, ranges of a round of workgroups, rounds at most
   size_t info, pm, pl, po, total;   // where sequences' partials lie; per unit and row: max, sum, output
 };
 PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16);

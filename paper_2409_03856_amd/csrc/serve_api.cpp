@@ -245,7 +245,7 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
   const int64_t rows = (int64_t)(H / Hkv) * cache->max_n;
   if (rows > INT32_MAX / 256) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
   const sirius::PagedAttnLayout L = sirius::paged_attn_layout(cache->B, cache->max_n, H, Hkv, hd, q_dtype == SIRIUS_BF16);
-  if ((int64_t)Hkv * L.rgroups * (cache->B + L.units) > INT32_MAX) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
+  if ((int64_t)Hkv * L.rgroups * (cache->B + L.rounds * L.units) > INT32_MAX) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
   if (ws_bytes < L.total) return fail(SIRIUS_EWORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, L.total);
   sirius::PagedAttnCall c{};
   c.q = q;
