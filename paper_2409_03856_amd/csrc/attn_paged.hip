@@ -80,13 +80,16 @@ __device__ __forceinline__ float exp_neg(float x) {
   return __builtin_amdgcn_exp2f(t) * fmaf(d, kLn2, 1.f);
 }
 
-// cap tanh(x / cap): the series of tanh up to 0.35 (the next term is 1e-8 of it), beyond it
-// 1 - 2 / (e^2a + 1).
+// cap tanh(x / cap) as x (1 - y^2 / 3 + ..), y = x / cap: the series of tanh, whose next term is 1e-8 at 0.35.
+__device__ __forceinline__ float cap_near(float x, float inv) {
+  const float y = x * inv, z = y * y;
+  return x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -8.86323553e-3f, 2.18694885e-2f), -5.39682540e-2f), 0.133333333f), -0.333333333f), 1.f);
+}
+// The same anywhere: beyond 0.35 cap 1 - 2 / (e^2y + 1).
 __device__ __forceinline__ float capped(float x, float cap, float inv) {
-  const float y = x * inv, a = fabsf(y), z = y * y;
-  float t = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -8.86323553e-3f, 2.18694885e-2f), -5.39682540e-2f), 0.133333333f), -0.333333333f), 1.f);
-  if (a > 0.35f) t = copysignf(1.f - 2.f / (__builtin_amdgcn_exp2f(fminf(a, 40.f) * 2.88539008f) + 1.f), y);
-  return y == y ? cap * t : y;
+  const float y = x * inv, a = fabsf(y);
+  const float far = cap * copysignf(1.f - 2.f / (__builtin_amdgcn_exp2f(fminf(a, 40.f) * 2.88539008f) + 1.f), y);
+  return a > 0.35f ? far : cap_near(x, inv);
 }
 
 // A workgroup's share: positions [c0, c1) of sequence b, whose first seen row is lo.
@@ -430,8 +433,16 @@ __device__ __forceinline__ void modify(const Args& a, float* x, const RowLimits&
   }
   if constexpr (MOD) {
     if (a.cap > 0.f) {
+      float most = fabsf(x[0]);
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = capped(x[e], a.cap, inv_cap);
+      for (int e = 1; e < N; ++e) most = __builtin_elementwise_maximum(most, fabsf(x[e]));
+      if (__ballot(!(most * inv_cap <= 0.35f)) != 0) {  // rare: scores are small beside a cap
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = capped(x[e], a.cap, inv_cap);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = cap_near(x[e], inv_cap);
+      }
     }
     if (a.slopes != nullptr) {
       const float away = (float)(lim.last - t0 - 8 * g);
