@@ -13,7 +13,7 @@
 // sample_chunk_kernel: one workgroup per chunk of a row, its logits in registers: the chunk's best
 // token, and what the row's filters need,
 //   few (1 < k <= 256)   the tokens that may be among the row's first k: those above a bound that at
-//                        least k of the chunk reach (the k-th of the maxima of 1024 groups);
+//                        least k of the chunk reach (the k-th of the maxima of 512 groups);
 //   other filters        the chunk's mass, and counts and masses by bins of an eighth of a temperature,
 //                        down to the lightest token that a cut can fall on;
 //   none                 the chunk's mass.
@@ -38,7 +38,7 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 constexpr int kTiles = 4096;      // tiles of a row at most
 constexpr int kTile = 1024;       // tokens per tile, a multiple of this where the row has more tiles
-constexpr int kChunkThreads = 256;
+constexpr int kMaximaAll = 512;   // groups of a chunk whose maxima bound its k-th token
 constexpr int kFew = 256;         // the largest k that goes by lists
 constexpr int kList = 512;        // entries of a chunk's list
 constexpr int kSort = 4096;       // tokens that are sorted in LDS at most
@@ -129,6 +129,13 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xffffffffu));
 }
 
+// The floats beside a finite one.
+__device__ __forceinline__ float next_up(float x) {
+  const int b = __float_as_int(x);
+  return x == 0.f ? __int_as_float(1) : __int_as_float(b > 0 ? b + 1 : b - 1);
+}
+__device__ __forceinline__ float next_down(float x) { return -next_up(-x); }
+
 // exp(z) for -700 <= z <= 0: the powers of two come off, the rest (at most ln 2 / 2) goes through the
 // series of exp, whose next term is 6e-15.
 __device__ __forceinline__ double exp_nonpos(double z) {
@@ -209,6 +216,11 @@ __device__ __forceinline__ void load4(const float* row, int V, int v0, float* x)
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = v0 + e < V ? row[v0 + e] : -INFINITY;
   }
+}
+
+__device__ __forceinline__ void load4_whole(const float* p, float* x) {
+  const float4 t = *reinterpret_cast<const float4*>(p);
+  x[0] = t.x; x[1] = t.y; x[2] = t.z; x[3] = t.w;
 }
 
 // A cut: tokens with keys above `key` stay, and the first `ties` of those that equal it.
@@ -474,17 +486,19 @@ __device__ __forceinline__ u64 fast_units(double y, int shift, const double* tab
   return (u64)__double_as_longlong(fma(t, g, t) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
-template <bool ALIGNED, int PER>
-__global__ __launch_bounds__(kChunkThreads, 4) void sample_chunk_kernel(Args a) {
-  constexpr int kW = kChunkThreads / kWave, kSub = 2;  // groups whose maxima bound the k-th token: 2 a thread
-  static_assert(kW == kMarks, "a bound for each wave");
+// THREADS * PER * 4 tokens; 256 threads with 8 float4s each stream a large call faster than 512 with 4 (18 against
+// 24 us for 98 MB), 512 with one each finish a small one sooner.
+template <bool ALIGNED, int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
+  constexpr int kW = THREADS / kWave, kSub = kMaximaAll / THREADS, kMaxima = kMaximaAll / kWave;
+  static_assert(kW >= kMarks && THREADS >= kFine, "a wave for each bound, a thread for each bin");
   __shared__ float s_x[kW], s_y[kW];
   __shared__ int s_i[kW], s_f[kW], s_n;
   __shared__ u64 s_m[kW];
   __shared__ uint32_t s_bound[kMarks];
   __shared__ int s_c[kW];
   __shared__ union {
-    uint32_t sub[kSub * kChunkThreads];
+    uint32_t sub[kMaximaAll];
     struct {
       double table[kTable];
       u64 mass[kFine];
@@ -498,103 +512,150 @@ __global__ __launch_bounds__(kChunkThreads, 4) void sample_chunk_kernel(Args a) 
   const float* row = a.logits + (long)b * a.ld;
   const int v0 = c * a.chunk;
   float x[PER][4];
+  if (ALIGNED && v0 + a.chunk <= a.V) {  // uniform: loads under no condition, all on their way together
 #pragma unroll
-  for (int j = 0; j < PER; ++j) load4<ALIGNED>(row, a.V, v0 + 4 * (tid + j * kChunkThreads), x[j]);
+    for (int j = 0; j < PER; ++j) load4_whole(row + v0 + 4 * (tid + j * THREADS), x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) load4<ALIGNED>(row, a.V, v0 + 4 * (tid + j * THREADS), x[j]);
+  }
+  if (q.mode == kNone) {  // greedy: the best and its index
+    float best = -INFINITY;
+    int at = INT32_MAX;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (x[j][e] > best) {
+          best = x[j][e];
+          at = v0 + 4 * (tid + j * THREADS) + e;
+        }
+    for (int o = 1; o < kWave; o <<= 1) {
+      const float ov = __shfl_xor(best, o, kWave);
+      const int oi = __shfl_xor(at, o, kWave);
+      if (ov > best || (ov == best && oi < at)) {
+        best = ov;
+        at = oi;
+      }
+    }
+    if (lane == 0) {
+      s_x[wave] = best;
+      s_i[wave] = at;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kW; ++w)
+        if (s_x[w] > best || (s_x[w] == best && s_i[w] < at)) {
+          best = s_x[w];
+          at = s_i[w];
+        }
+      a.stat[(size_t)b * a.chunks + c] = ChunkStat{best, best, at, 0, 0, {}, 0};
+    }
+    return;
+  }
+  const bool sums = q.mode == kByBins || q.mode == kWhole;  // uniform
   float best = -INFINITY, least = INFINITY;
-  int at = INT32_MAX, finite = 0;
 #pragma unroll
   for (int j = 0; j < PER; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float& y = x[j][e];
-      if (!(y > -INFINITY)) y = -INFINITY;  // NaN too
-      if (y > best) {
-        best = y;
-        at = v0 + 4 * (tid + j * kChunkThreads) + e;
-      }
-      if (y > -INFINITY) {
-        ++finite;
-        least = fminf(least, y);
-      }
+      x[j][e] = fmaxf(x[j][e], -INFINITY);  // a NaN too
+      best = fmaxf(best, x[j][e]);
+      least = fminf(least, x[j][e]);
     }
   for (int o = 1; o < kWave; o <<= 1) {
-    const float ov = __shfl_xor(best, o, kWave);
-    const int oi = __shfl_xor(at, o, kWave);
-    if (ov > best || (ov == best && oi < at)) {
-      best = ov;
-      at = oi;
-    }
+    best = fmaxf(best, __shfl_xor(best, o, kWave));
     least = fminf(least, __shfl_xor(least, o, kWave));
-    finite += __shfl_xor(finite, o, kWave);
   }
   if (lane == 0) {
     s_x[wave] = best;
     s_y[wave] = least;
-    s_i[wave] = at;
-    s_f[wave] = finite;
   }
   if (tid == 0) s_n = 0;
-  if (q.mode == kByBins || q.mode == kWhole) fill_table(sh.table);
-  if (q.mode == kByBins) {
+  if (sums) fill_table(sh.table);
+  if (q.mode == kByBins && tid < kFine) {
     sh.mass[tid] = 0;
     sh.count[tid] = 0;
   }
   if (q.mode == kByList) {
 #pragma unroll
-    for (int k = 0; k < kSub; ++k) {
+    for (int k = 0; k < kSub; ++k) {  // of the thread's tokens, in kSub groups
       float m = -INFINITY;
 #pragma unroll
       for (int e = k * 4 * PER / kSub; e < (k + 1) * 4 * PER / kSub; ++e) m = fmaxf(m, x[e / 4][e % 4]);
-      sh.sub[k * kChunkThreads + tid] = key_of(m);
+      sh.sub[k * THREADS + tid] = key_of(m);
     }
   }
   __syncthreads();
-  best = s_x[0];
-  at = s_i[0];
-  least = s_y[0];
-  finite = s_f[0];
-  for (int w = 1; w < kW; ++w) {
-    if (s_x[w] > best || (s_x[w] == best && s_i[w] < at)) {
-      best = s_x[w];
-      at = s_i[w];
-    }
+#pragma unroll
+  for (int w = 0; w < kW; ++w) {
+    best = fmaxf(best, s_x[w]);
     least = fminf(least, s_y[w]);
-    finite += s_f[w];
   }
-  ChunkStat st{best, least, at, finite, 0, {}, 0};
+  int finite = min(a.V, v0 + a.chunk) - v0;
+  if (sums && least == -INFINITY) {  // uniform: what is finite, and the least of it
+    float low = INFINITY;
+    finite = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (x[j][e] > -INFINITY) {
+          ++finite;
+          low = fminf(low, x[j][e]);
+        }
+    for (int o = 1; o < kWave; o <<= 1) {
+      low = fminf(low, __shfl_xor(low, o, kWave));
+      finite += __shfl_xor(finite, o, kWave);
+    }
+    __syncthreads();
+    if (lane == 0) {
+      s_y[wave] = low;
+      s_f[wave] = finite;
+    }
+    __syncthreads();
+    least = s_y[0];
+    finite = 0;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+      least = fminf(least, s_y[w]);
+      finite += s_f[w];
+    }
+  }
+  ChunkStat st{best, least, INT32_MAX, finite, 0, {}, 0};
   u64* list = a.list + ((size_t)b * a.chunks + c) * kList;
   if (q.mode == kByList) {
-    {  // the largest key of 16 bits that so many of the groups' maxima reach
+    if (wave < kMarks) {  // the largest key of 16 bits that so many of the threads' maxima reach
       const int want = mark_of(q.top_k, wave);
-      uint32_t sub[kSub * kW];
+      uint32_t sub[kMaxima];
 #pragma unroll
-      for (int k = 0; k < kSub * kW; ++k) sub[k] = sh.sub[k * kWave + lane];
+      for (int k = 0; k < kMaxima; ++k) sub[k] = sh.sub[k * kWave + lane];
       uint32_t bound = 0;
       for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
         int n = 0;
 #pragma unroll
-        for (int k = 0; k < kSub * kW; ++k) n += __popcll(__ballot(sub[k] >= (bound | bit)));
+        for (int k = 0; k < kMaxima; ++k) n += __popcll(__ballot(sub[k] >= (bound | bit)));
         if (n >= want) bound |= bit;
       }
       if (lane == 0) s_bound[wave] = bound;
     }
     __syncthreads();
     const uint32_t bound = s_bound[0];
+    const float reach = bound > key_of(-INFINITY) ? logit_of(bound) : -INFINITY;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t key = key_of(x[j][e]);
-        if (key >= bound && x[j][e] > -INFINITY) {
+        if (x[j][e] >= reach && x[j][e] > -INFINITY) {
           const int n = atomicAdd(&s_n, 1);
-          if (n < kList) list[n] = (u64)key << 32 | ~(uint32_t)(v0 + 4 * (tid + j * kChunkThreads) + e);
+          if (n < kList) list[n] = (u64)key_of(x[j][e]) << 32 | ~(uint32_t)(v0 + 4 * (tid + j * THREADS) + e);
         }
       }
     __syncthreads();
     st.listed = s_n;
 #pragma unroll
     for (int i = 0; i < kMarks; ++i) st.bound[i] = s_bound[i] > key_of(-INFINITY) ? s_bound[i] : 0;
-  } else if (q.mode != kNone && best > -INFINITY) {
+  } else if (sums && best > -INFINITY) {
     const double to = kTable * 1.44269504088896340736 / (double)q.temp, from = (double)best;
     const float s = bin_scale(q), top = bin_of(best, s);
     const float last = q.mode == kByBins ? (float)last_bin(q, a.V) : -1.f;
@@ -622,8 +683,8 @@ __global__ __launch_bounds__(kChunkThreads, 4) void sample_chunk_kernel(Args a) 
     __syncthreads();
     for (int w = 0; w < kW; ++w) st.mass += s_m[w];
     if (q.mode == kByBins) {  // sums up to each bin's end
-      u64 cm = sh.mass[tid];
-      int cc = sh.count[tid];
+      u64 cm = tid < kFine ? sh.mass[tid] : 0;
+      int cc = tid < kFine ? (int)sh.count[tid] : 0;
       for (int o = 1; o < kWave; o <<= 1) {
         const u64 om = shfl_up64(cm, o);
         const int oc = __shfl_up(cc, o, kWave);
@@ -642,8 +703,10 @@ __global__ __launch_bounds__(kChunkThreads, 4) void sample_chunk_kernel(Args a) 
         cm += s_m[w];
         cc += s_c[w];
       }
-      list[tid] = cm;
-      reinterpret_cast<uint32_t*>(list + kFine)[tid] = cc;
+      if (tid < kFine) {
+        list[tid] = cm;
+        reinterpret_cast<uint32_t*>(list + kFine)[tid] = cc;
+      }
     }
   }
   if (tid == 0) a.stat[(size_t)b * a.chunks + c] = st;
@@ -875,7 +938,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     total = block_scan(0, total, sh.scan_c, sh.scan_m).mt;
     {  // half of the threads each take every second chunk of a bin
       static_assert(kThreads == 2 * kFine, "two threads a bin");
-      constexpr int kAhead = 8;
+      constexpr int kAhead = 16;
       const int bin = tid & (kFine - 1);
       u64 m = 0;
       int n = 0;
@@ -936,40 +999,77 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       __syncthreads();
       above_c = sh.cum_count[b0];
       above = sh.cum_mass[b0];
-      constexpr int kAhead = 8;
-      for (int c = wave; c < a.chunks; c += kWaves) {
-        if (!(sh.off[c] <= (float)b1)) continue;
-        const int end = min(V, (c + 1) * a.chunk);
-        for (int v0 = c * a.chunk + 4 * lane; v0 - 4 * lane < end; v0 += 4 * kAhead * kWave) {  // whole waves
-          float x[kAhead][4];
+      // Pieces of 2048 tokens, one wave each; the next piece is on its way while one is looked through. Chunks
+      // whose best lies behind the bins are passed over.
+      constexpr int kAhead = 8, kPiece = 4 * kAhead * kWave;
+      const int pieces = (V + kPiece - 1) / kPiece;
+      auto next = [&](int p) {
+        while (p < pieces && !(sh.off[p * kPiece / a.chunk] <= (float)b1)) p += kWaves;
+        return p;
+      };
+      auto fetch = [&](int p, float (&x)[kAhead][4]) {
+        if (ALIGNED && (p + 1) * kPiece <= V) {  // uniform: loads under no condition, all on their way together
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) load4<ALIGNED>(row, v0 + 4 * k * kWave < end ? V : 0, v0 + 4 * k * kWave, x[k]);
-          uint32_t hits = 0;
-          static_assert(4 * kAhead == 32, "a bit for each");
+          for (int k = 0; k < kAhead; ++k) load4_whole(row + p * kPiece + 4 * (lane + k * kWave), x[k]);
+        } else {
 #pragma unroll
-          for (int k = 0; k < 4 * kAhead; ++k) {
-            const float y = x[k >> 2][k & 3], bin = top - bin_of(y, s);
-            if (bin >= (float)b0 && bin <= (float)b1) hits |= 1u << k;  // no NaN, no infinity
-          }
-          const int mine = __popc(hits);
-          int upto = mine;
-          for (int o = 1; o < kWave; o <<= 1) {
-            const int t = __shfl_up(upto, o, kWave);
-            if (lane >= o) upto += t;
-          }
-          int to = 0;
-          if (lane == kWave - 1 && upto > 0) to = atomicAdd(&sh.n, upto);
-          to = __shfl(to, kWave - 1, kWave) + upto - mine;
-#pragma unroll
-          for (int k = 0; k < 4 * kAhead; ++k)
-            if ((hits >> k & 1u) != 0) {
-              if (to < kSort) sh.sorted[to] = (u64)key_of(x[k >> 2][k & 3]) << 32 | ~(uint32_t)(v0 + (k >> 2) * 4 * kWave + (k & 3));
-              ++to;
-            }
+          for (int k = 0; k < kAhead; ++k) load4<ALIGNED>(row, p < pieces ? V : 0, p * kPiece + 4 * (lane + k * kWave), x[k]);
         }
+      };
+      // The bins as a range of logits: the outermost ones that floor(x s) puts there
+      float low = (top - (float)b1) / s, high = (top - (float)b0 + 1.f) / s;
+      while (!(top - bin_of(low, s) <= (float)b1)) low = next_up(low);
+      while (top - bin_of(next_down(low), s) <= (float)b1) low = next_down(low);
+      while (!(top - bin_of(high, s) >= (float)b0)) high = next_down(high);
+      while (top - bin_of(next_up(high), s) >= (float)b0) high = next_up(high);
+      // each wave lists what it finds in its own part of the room; one that runs over sends the row the long way
+      constexpr int kRoom = kSort / kWaves;
+      int found = 0;
+      auto look = [&](int p, const float (&x)[kAhead][4]) {
+#pragma unroll
+        for (int k = 0; k < 4 * kAhead; ++k) {
+          const float y = x[k >> 2][k & 3];
+          const bool in = (y >= low) & (y <= high);  // no NaN, no infinity
+          const uint64_t hit = __ballot(in);
+          if (hit == 0) continue;  // uniform
+          const int at = found + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+          if (in && at < kRoom)
+            sh.sorted[wave * kRoom + at] = (u64)key_of(y) << 32 | ~(uint32_t)(p * kPiece + 4 * (lane + (k >> 2) * kWave) + (k & 3));
+          found += __popcll(hit);
+        }
+      };
+      float xa[kAhead][4], xb[kAhead][4];
+      int p = next(wave);
+      fetch(p, xa);
+      while (p < pieces) {
+        const int p2 = next(p + kWaves);
+        fetch(p2, xb);
+        look(p, xa);
+        if (p2 >= pieces) break;
+        p = next(p2 + kWaves);
+        fetch(p, xa);
+        look(p2, xb);
+      }
+      if (lane == 0) sh.i[wave] = found;
+      __syncthreads();
+      u64 mine[kRoom / kWave];  // the parts moved together
+#pragma unroll
+      for (int k = 0; k < kRoom / kWave; ++k) mine[k] = sh.sorted[wave * kRoom + k * kWave + lane];
+      int from = 0, n = 0;
+      bool over = false;
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) from += sh.i[w];
+        n += sh.i[w];
+        over |= sh.i[w] > kRoom;
       }
       __syncthreads();
-      return sh.n <= kSort;
+      if (over) return false;
+#pragma unroll
+      for (int k = 0; k < kRoom / kWave; ++k)
+        if (k * kWave + lane < found) sh.sorted[from + k * kWave + lane] = mine[k];
+      if (tid == 0) sh.n = n;
+      __syncthreads();
+      return true;
     };
     // The last of the gathered tokens (in order) that stays and how many do, by count (want > 0: of them) or by
     // the mass in front (share): counts and masses by 256 steps of the keys, then the tokens of the step
@@ -1215,11 +1315,11 @@ hipError_t launch_sample(const SampleCall& c, char* ws, const SampleLayout& L, h
     ProfScope prof("sample_chunk", stream);
     const int grid = c.B * a.chunks;
     if (a.chunk == 2048) {
-      if (aligned) klaunch(sample_chunk_kernel<true, 2>, grid, kChunkThreads, 0, stream, a);
-      else klaunch(sample_chunk_kernel<false, 2>, grid, kChunkThreads, 0, stream, a);
+      if (aligned) klaunch(sample_chunk_kernel<true, 512, 1>, grid, 512, 0, stream, a);
+      else klaunch(sample_chunk_kernel<false, 512, 1>, grid, 512, 0, stream, a);
     } else {
-      if (aligned) klaunch(sample_chunk_kernel<true, 8>, grid, kChunkThreads, 0, stream, a);
-      else klaunch(sample_chunk_kernel<false, 8>, grid, kChunkThreads, 0, stream, a);
+      if (aligned) klaunch(sample_chunk_kernel<true, 256, 8>, grid, 256, 0, stream, a);
+      else klaunch(sample_chunk_kernel<false, 256, 8>, grid, 256, 0, stream, a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
