@@ -362,21 +362,22 @@ __device__ __forceinline__ void whole_row(const Args& a, const Unit& u, int r, i
   }
 }
 
-// A sequence outside its table, or a page outside the pool: NaN for its rows of this head.
+// A sequence outside its table, or a page outside the pool: NaN for its rows r0 .. r1 - 1 of this head (r1 may be
+// beyond what an int holds: a sequence may have more tokens than the call was made for).
 template <typename TQ>
-__device__ __forceinline__ void not_a_number(const Args& a, const Unit& u, int kvh, int r0, int r1, int R) {
+__device__ __forceinline__ void not_a_number(const Args& a, const Unit& u, int kvh, long r0, long r1, int R) {
   const int tid = threadIdx.x;
   if (u.count > 1) {
-    for (int r = r0 + tid; r < r1; r += kThreads) {
+    for (long r = r0 + tid; r < r1; r += kThreads) {
       const size_t row = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R + r;
       a.pm[row] = 0.f;
       a.pl[row] = __builtin_nanf("");
     }
     return;
   }
-  for (int e = tid; e < (r1 - r0) * a.hd; e += kThreads) {
-    const int r = r0 + e / a.hd, i = r / a.G, h = kvh * a.G + (r - i * a.G);
-    put(static_cast<TQ*>(a.out) + ((long)(u.first + i) * a.H + h) * a.hd + e % a.hd, __builtin_nanf(""));
+  for (long e = tid; e < (r1 - r0) * a.hd; e += kThreads) {
+    const long r = r0 + e / a.hd, i = r / a.G, h = kvh * a.G + (r - i * a.G);
+    put(static_cast<TQ*>(a.out) + ((u.first + i) * a.H + h) * a.hd + e % a.hd, __builtin_nanf(""));
   }
 }
 
@@ -470,13 +471,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_rows_kernel(Args a) {
   const int kvh = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv % a.rgroups;
   const Unit u = unit_at(a, make_plan(a), blockIdx.x / (a.Hkv * a.rgroups));
   if (u.b < 0) return;
-  const int R = a.G * a.pg.n, r0 = rg * 16, nrows = u.n * a.G;
+  const int R = a.G * a.pg.n, r0 = rg * 16;
   if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
   if (u.c1 <= u.c0 && !valid(a, u.p, u.n)) {
     // every row, also those behind the row groups that the call was launched for
-    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, nrows, R);
+    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, (long)u.n * a.G, R);
     return;
   }
+  const int nrows = u.n * a.G;
   if (r0 >= nrows) return;
   const int nr = min(16, nrows - r0);
   const size_t prow = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R + r0;  // this unit's partial rows
@@ -726,12 +728,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   const int kvh = blockIdx.x % a.Hkv, rg = a.rgroups - 1 - blockIdx.x / a.Hkv % a.rgroups;
   const Unit u = unit_at(a, make_plan(a), blockIdx.x / (a.Hkv * a.rgroups));
   if (u.b < 0) return;
-  const int R = a.G * a.pg.n, r0 = rg * 64 * QT, nrows = u.n * a.G;
+  const int R = a.G * a.pg.n, r0 = rg * 64 * QT;
   if (tid == 0 && kvh == 0 && rg == 0) a.info[u.b] = make_int2(u.slot, u.count);
   if (u.c1 <= u.c0 && !valid(a, u.p, u.n)) {
-    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, nrows, R);
+    if (rg == 0) not_a_number<TQ>(a, u, kvh, 0, (long)u.n * a.G, R);
     return;
   }
+  const int nrows = u.n * a.G;
   if (r0 >= nrows) return;
   const int nr = min(64 * QT, nrows - r0);
   const size_t prow = ((size_t)(u.slot + u.part) * a.Hkv + kvh) * R;

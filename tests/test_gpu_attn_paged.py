@@ -226,6 +226,16 @@ def test_ragged_batch_long_and_short(sr):
     _parity(sr, 31, before, new, 16, 2, 1, 64, "f32", max_n=3)
 
 
+@pytest.mark.parametrize("qt", ["f32", "bf16"])
+@pytest.mark.parametrize("before,new,page,h,hkv,hd", [
+    ([24000, 16500], [1, 1], 16, 64, 64, 8),    # units longer than the pages staged at once
+    ([5000], [600], 24, 64, 64, 8),             # whole sequences in tiles, their page ring wraps
+    ([3000, 2500, 3100], [20, 20, 20], 8, 64, 64, 8),
+])
+def test_long_units(sr, qt, before, new, page, h, hkv, hd):
+    _parity(sr, 40 + hd, before, new, page, h, hkv, hd, qt, max_n=max(new))
+
+
 def test_strided_queries_and_streams(sr):
     import torch
     before, new, page = [300, 20], [3, 3], 16
