@@ -579,9 +579,9 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
  *   ones with w >= m; the best one always.
  * The token is the first one in index order whose running kept mass exceeds u times the kept
  * mass (u is clamped to [0, 1]; at 1 the last kept token of positive mass).
- * Weights hold at least 33 bits and are added as whole numbers of 2^-min(50, 62 - ceil(log2 V)) of the best
- * one's, so a call's result does not depend on the order of its sums.
- *   logits [B, V] fp32, rows ld elements apart (ld >= V; 16-byte aligned base).
+ * Weights are within 1e-13 of their value and are added as whole numbers of
+ * 2^-min(50, 62 - ceil(log2 V)) of the best one's, so a call's result does not depend on the order of its sums.
+ *   logits [B, V] fp32, rows ld elements apart (V <= ld <= 2^31; 16-byte aligned base).
  *   u      [B] fp32.
  *   temperature [B] fp32 or NULL (1); 0 is greedy: the argmax, lowest index on ties.
  *   top_k  [B] int32 or NULL; <= 0 or >= V: off.
@@ -592,7 +592,7 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
  * A row without a logit above -infinity, and one with a NaN parameter, a negative or an infinite
  * temperature, gives token -1, kept 0, prob 0. Needs sirius_workspace_size(SIRIUS_OP_SAMPLE, ...).
  * B == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null pointers (where not allowed above), B
- * outside [0, 65535], V outside [1, 2^24], ld < V, misaligned logits; SIRIUS_EWORKSPACE.
+ * outside [0, 65535], V outside [1, 2^24], ld outside [V, 2^31], misaligned logits; SIRIUS_EWORKSPACE.
  */
 int sirius_sample(const float* logits, int64_t ld, int B, int V, const float* u,
                   const float* temperature, const int32_t* top_k, const float* top_p,

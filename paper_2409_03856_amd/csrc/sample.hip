@@ -129,12 +129,30 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xffffffffu));
 }
 
-// The floats beside a finite one.
-__device__ __forceinline__ float next_up(float x) {
-  const int b = __float_as_int(x);
-  return x == 0.f ? __int_as_float(1) : __int_as_float(b > 0 ? b + 1 : b - 1);
+// The first key of a finite logit for which `reached` holds, as it does for all behind it; 64 keys at a time, one per
+// lane. Infinity's key: none.
+template <typename F>
+__device__ __forceinline__ uint32_t first_key(F reached) {
+  constexpr uint32_t kLast = 0xff7fffffu;
+  const uint32_t lane = threadIdx.x & (kWave - 1);
+  uint32_t base = 0x00800000u;  // the lowest logit's; later one that is not reached
+  for (int bits = 26; bits >= 0; bits = bits > 6 ? bits - 6 : bits - 2) {  // 26, 20, 14, 8, 2, 0
+    const uint32_t away = lane << bits, key = away > kLast - base ? kLast : base + away;
+    const int n = __popcll(__ballot(!reached(logit_of(key))));  // of lanes in order
+    if (bits == 0) return min(base + n, kLast + 1);
+    const uint32_t on = (uint32_t)max(n - 1, 0) << bits;
+    if (on > kLast - base) break;
+    base += on;
+  }
+  return kLast + 1;
 }
-__device__ __forceinline__ float next_down(float x) { return -next_up(-x); }
+
+// Lighter than exp(-`least`) beside the best (NaN too). What lies kNothing temperatures below it weighs nothing; up to
+// kClear nobody has to look.
+constexpr double kNothing = 700.0, kClear = 690.0;
+__device__ __forceinline__ bool far_below(float x, double best, double inv_t, double least) {
+  return !(((double)x - best) * inv_t >= -least);
+}
 
 // exp(z) for -700 <= z <= 0: the powers of two come off, the rest (at most ln 2 / 2) goes through the
 // series of exp, whose next term is 6e-15.
@@ -160,11 +178,9 @@ __device__ __forceinline__ double exp_nonpos(double z) {
 struct Weigh {
   double best, inv_t;
   int shift;
-  // 0 for what weighs nothing: more than 700 temperatures below the best
   __device__ __forceinline__ double weight(float x) const {
     if (best == INFINITY) return x == INFINITY ? 1.0 : 0.0;
-    const double z = ((double)x - best) * inv_t;
-    return z >= -700.0 ? exp_nonpos(z) : 0.0;  // NaN too
+    return far_below(x, best, inv_t, kNothing) ? 0.0 : exp_nonpos(((double)x - best) * inv_t);
   }
   __device__ __forceinline__ u64 units(double w) const { return (u64)rint(ldexp(w, shift)); }
 };
@@ -593,17 +609,19 @@ __global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
     least = fminf(least, s_y[w]);
   }
   int finite = min(a.V, v0 + a.chunk) - v0;
-  if (sums && least == -INFINITY) {  // uniform: what is finite, and the least of it
+  if (const double inv_t = 1.0 / (double)q.temp; sums && far_below(least, (double)best, inv_t, kClear)) {
+    // uniform: what weighs something beside the chunk's best, and the least of it; a mask's lowest numbers are not counted
     float low = INFINITY;
     finite = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (x[j][e] > -INFINITY) {
+      for (int e = 0; e < 4; ++e) {
+        if (!far_below(x[j][e], (double)best, inv_t, kNothing)) {
           ++finite;
           low = fminf(low, x[j][e]);
         }
+      }
     for (int o = 1; o < kWave; o <<= 1) {
       low = fminf(low, __shfl_xor(low, o, kWave));
       finite += __shfl_xor(finite, o, kWave);
@@ -641,7 +659,9 @@ __global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
     }
     __syncthreads();
     const uint32_t bound = s_bound[0];
-    const float reach = bound > key_of(-INFINITY) ? logit_of(bound) : -INFINITY;
+    float reach = bound > key_of(-INFINITY) ? logit_of(bound) : -INFINITY;
+    // tokens that weigh nothing stay off the list: few may be left where a mask's lowest numbers are many
+    reach = fmaxf(reach, (float)((double)best - (kNothing + 1.0) * (double)q.temp));
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
@@ -769,10 +789,9 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     if (tid == 0) answer(-1, 0, 0.f);
     return;
   }
-  // ---- the row's best, its least finite logit and their number; lists that overflowed
+  // ---- the row's best, the least logit that its chunks count and how many those are
   float best = -INFINITY, least = INFINITY;
   int at = INT32_MAX, finite = 0;
-  bool over = false;
   for (int c = tid; c < a.chunks; c += kThreads) {
     const ChunkStat st = stat[c];
     if (st.best > best || (st.best == best && st.best_at < at)) {
@@ -781,7 +800,6 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     }
     least = fminf(least, st.least);
     finite += st.finite;
-    over |= q.mode == kByList && st.listed > kList;
   }
   if (a.chunks > 1) {  // uniform
     for (int o = 1; o < kWave; o <<= 1) {
@@ -795,12 +813,11 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       finite += __shfl_xor(finite, o, kWave);
     }
   }
-  over = __ballot(over) != 0;
   if (lane == 0) {
     sh.x[wave] = best;
     sh.i[wave] = at;
     sh.scan_c[wave] = finite;
-    sh.scan_m[wave] = (u64)__float_as_uint(least) << 32 | (over ? 1 : 0);
+    sh.scan_m[wave] = __float_as_uint(least);
   }
   if (tid == 0) {
     sh.n = 0;
@@ -811,16 +828,14 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   best = sh.x[0];
   at = sh.i[0];
   finite = sh.scan_c[0];
-  least = __uint_as_float((uint32_t)(sh.scan_m[0] >> 32));
-  over = (uint32_t)sh.scan_m[0] != 0;
+  least = __uint_as_float((uint32_t)sh.scan_m[0]);
   for (int w = 1; w < nw; ++w) {
     if (sh.x[w] > best || (sh.x[w] == best && sh.i[w] < at)) {
       best = sh.x[w];
       at = sh.i[w];
     }
     finite += sh.scan_c[w];
-    least = fminf(least, __uint_as_float((uint32_t)(sh.scan_m[w] >> 32)));
-    over |= (uint32_t)sh.scan_m[w] != 0;
+    least = fminf(least, __uint_as_float((uint32_t)sh.scan_m[w]));
   }
   if (best == -INFINITY || q.greedy) {
     if (tid == 0) {
@@ -832,8 +847,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   const Weigh wg{(double)best, 1.0 / (double)q.temp, a.shift};
   const double share_u = (double)fminf(fmaxf(q.u, 0.f), 1.f);
   const float s = bin_scale(q), top = bin_of(best, s);
-  // infinite logits; lists that overflowed
-  bool longway = best == INFINITY || over;
+  bool longway = best == INFINITY;
   if (q.mode == kByList && !longway) {
     if (wave == 0) {
       // The largest key that k tokens of the row are known to reach: the chunks' bounds say how many of
@@ -869,7 +883,13 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = min(c0 + k * kWaves, a.chunks - 1);
-        n[k] = c0 + k * kWaves < a.chunks ? stat[c].listed : 0;
+        // a list without a token that reaches the bound is passed over, also one that overflowed
+        const int listed = stat[c].listed;
+        n[k] = (c0 + k * kWaves < a.chunks) & (key_of(stat[c].best) >= bound) ? listed : 0;
+        if (n[k] > kList) {
+          if (lane == 0) atomicAdd(&sh.n, kSort + 1);  // the long way
+          n[k] = 0;
+        }
         e[k] = a.list[((size_t)b * a.chunks + c) * kList + lane];
       }
 #pragma unroll
@@ -911,15 +931,46 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
       return;
     }
   }
-  // Beside the best a token may weigh nothing although its chunk counted it, and bins have to be exact.
-  if (((double)best - (double)least) * wg.inv_t > 690.0 || !(fabsf(top) < 8388608.f) || !(fabsf(bin_of(least, s)) < 8388608.f)) longway = true;
+  if (!(fabsf(top) < 8388608.f)) longway = true;  // the bins beside it have to be exact
+  if (!longway && far_below(least, wg.best, wg.inv_t, kClear)) {
+    // Beside the row's best a token may weigh nothing although its chunk counted it. Whole chunks leave first, then the
+    // row is counted (8 cold rows of 128256 tokens: 21 us, against 8 at a temperature where no token is so far below).
+    auto add_up = [&]() {
+      const int n = block_scan(finite, 0, sh.scan_c, sh.scan_m).ct;
+      __syncthreads();
+      for (int o = 1; o < kWave; o <<= 1) least = fminf(least, __shfl_xor(least, o, kWave));
+      if (lane == 0) sh.x[wave] = least;
+      __syncthreads();
+      for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.x[w]);
+      finite = n;
+    };
+    least = INFINITY;
+    finite = 0;
+    for (int c = tid; c < a.chunks; c += kThreads) {
+      const ChunkStat st = stat[c];
+      if (far_below(st.best, wg.best, wg.inv_t, kNothing)) continue;
+      least = fminf(least, st.least);
+      finite += st.finite;
+    }
+    add_up();
+    if (far_below(least, wg.best, wg.inv_t, kClear)) {
+      finite = 0;
+      for (int v0 = 4 * tid; v0 < V; v0 += 4 * kThreads) {
+        float x[4];
+        load4<ALIGNED>(row, V, v0, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) finite += far_below(x[e], wg.best, wg.inv_t, kNothing) ? 0 : 1;
+      }
+      add_up();
+    }
+  }
   // a mass in units of a chunk's best, in the row's
   auto scaled = [&](u64 m, int c) { return (u64)rint((double)m * sh.scale[c]); };
   if (!longway && q.mode != kByList) {
     __syncthreads();
     for (int c = tid; c < a.chunks; c += kThreads) {
       const float from = stat[c].best;
-      const bool has = from > -INFINITY;
+      const bool has = !far_below(from, wg.best, wg.inv_t, kNothing);
       sh.off[c] = has ? top - bin_of(from, s) : INFINITY;
       sh.scale[c] = has ? exp_nonpos(((double)from - (double)best) * wg.inv_t) : 0.0;
     }
@@ -1017,11 +1068,8 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
         }
       };
       // The bins as a range of logits: the outermost ones that floor(x s) puts there
-      float low = (top - (float)b1) / s, high = (top - (float)b0 + 1.f) / s;
-      while (!(top - bin_of(low, s) <= (float)b1)) low = next_up(low);
-      while (top - bin_of(next_down(low), s) <= (float)b1) low = next_down(low);
-      while (!(top - bin_of(high, s) >= (float)b0)) high = next_down(high);
-      while (top - bin_of(next_up(high), s) >= (float)b0) high = next_up(high);
+      const float low = logit_of(first_key([&](float x) { return top - bin_of(x, s) <= (float)b1; }));
+      const float high = logit_of(first_key([&](float x) { return top - bin_of(x, s) < (float)b0; }) - 1);
       // each wave lists what it finds in its own part of the room; one that runs over sends the row the long way
       constexpr int kRoom = kSort / kWaves;
       int found = 0;

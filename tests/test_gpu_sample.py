@@ -143,6 +143,59 @@ def test_masked_infinite_and_nan_logits(sr):
         assert tok[1] == -1 and tok[2] == -1 and tok[4] in (7, 4000) and tok[5] == 0 and tok[6] == 123
 
 
+def test_masks_of_the_lowest_value_and_cold_rows(sr):
+    """Tokens that weigh nothing (a mask's finite numbers, cold temperatures) are in no count, whatever share of a
+    chunk or of the row they are; the end of the row masked as a padded vocabulary is."""
+    rng = np.random.default_rng(15)
+    v = 20000
+    x = _logits(rng, 8, v)
+    low = np.finfo(np.float32).min
+    x[0, rng.random(v) < 0.5] = low
+    x[1, 9000:] = low
+    x[2, rng.random(v) < 0.999] = -1e9
+    x[3, 16000:] = -1e4
+    x[4, :8192] = low
+    x[4, 8192:] -= 400.0
+    x[5, ::2] -= 350.0
+    x[5, 1::4] -= 695.0
+    x[6, 1000:] = -np.inf
+    x[6, ::7] = low
+    u = rng.random(8).astype(np.float32)
+    f = lambda a: np.full(8, a, np.float32)
+    for t, k, p, m in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.05), (1.0, 300, 1.0, 0.0), (1.0, 300, 0.8, 0.01),
+                       (0.01, 0, 1.0, 0.0), (0.01, 0, 0.95, 0.0), (0.01, 300, 0.95, 0.0), (0.003, 0, 1.0, 0.001), (1.0, 40, 0.9, 0.0),
+                       (1.0, 3, 1.0, 0.0), (1.0, 256, 1.0, 0.0), (0.01, 200, 1.0, 0.0)):
+        _check(sr, x, u, f(t), np.full(8, k), f(p), f(m))
+
+
+def test_cuts_beside_zero_at_hot_temperatures(sr):
+    """All logits in one bin around zero, whose products with a hot temperature's scale vanish."""
+    rng = np.random.default_rng(16)
+    x = rng.standard_normal((5, 400)).astype(np.float32)
+    x[1] = np.abs(x[1])
+    x[2] = -np.abs(x[2])
+    x[3] = rng.choice(np.array([0.0, -0.0, 1e-45, -1e-45, 1e-40, -1e-38], np.float32), 400)
+    x[4] *= 1e30
+    u = rng.random(5).astype(np.float32)
+    for t in (1e3, 1e12, 1e30, 3e38):
+        for k, p, m in ((0, 0.5, 0.0), (0, 1.0, 0.9), (300, 0.7, 0.5)):
+            _check(sr, x, u, np.full(5, t, np.float32), np.full(5, k), np.full(5, p, np.float32), np.full(5, m, np.float32))
+
+
+def test_rows_beyond_32_bits(sr):
+    """Rows so far apart that their offsets pass 2^32 elements; further apart than 2^31 they are refused."""
+    import torch
+    rng = np.random.default_rng(17)
+    x = _logits(rng, 3, 5000)
+    buf = torch.empty(2 * 2_200_000_000 + 5000, dtype=torch.float32, device="cuda")
+    X = buf.as_strided((3, 5000), (2_200_000_000, 1))
+    with pytest.raises(sr.SiriusError, match="apart"):
+        sr.sirius_sample(X, dev_f32(np.zeros(3)))
+    X = buf.as_strided((3, 5000), (2 ** 31, 1))
+    X.copy_(dev_f32(x))
+    _check(sr, x, rng.random(3), np.full(3, 0.9, np.float32), np.array([0, 20, 300]), np.array([0.9, 0.9, 1.0], np.float32), None, X=X)
+
+
 def test_bad_parameters_give_no_token(sr):
     x = np.zeros((7, 10), np.float32)
     t = np.array([-1, np.nan, np.inf, 1, 1, 1, 1], np.float32)

@@ -221,3 +221,31 @@ def test_two_streams_and_two_threads(sr):
         t.join(60)
     for a, b in zip(found, want):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_pages_beyond_32_bits(sr):
+    """Pages whose elements lie beyond 2^32: what is appended there and read back is bit for bit a small pool's."""
+    import torch
+    rng = np.random.default_rng(9)
+    hkv, hd, page = 8, 128, 64
+    high = 2 ** 32 // (hkv * hd * page) + 3
+    used = [high - 1, 0, high - 2, 1, high // 2 + 1, high - 3]
+    shape = {"k": (hkv, page, hd), "v": (hkv, hd, page)}
+    pos, start = np.array([70, 100], np.int32), np.array([0, 50, 51], np.int32)
+    q = rng.standard_normal((51, 16, hd)).astype(np.float32)
+    k, v = (bf16_bits(rng.standard_normal((51, hkv, hd)).astype(np.float32)) for _ in range(2))
+    old = {n: dev_bf16(bf16_bits(rng.standard_normal((6,) + shape[n]).astype(np.float32))) for n in "kv"}
+    got = []
+    for ids, pages in ((used, high), (list(range(6)), 6)):
+        pools = {n: torch.empty((pages,) + shape[n], dtype=torch.bfloat16, device="cuda") for n in "kv"}
+        for n in "kv":
+            for j, i in enumerate(ids):
+                pools[n][i].copy_(old[n][j])
+        table = dev_i32(np.array([ids[:3], ids[3:]], np.int32))
+        kv = (pools["k"], pools["v"], table, dev_i32(pos))
+        qr = sr.sirius_kv_append(dev_f32(q), dev_bf16(k), dev_bf16(v), *kv, sr.sirius_rope_freqs(hd, 10000.0), tok_start=dev_i32(start))
+        out = sr.sirius_attn_paged(qr, *kv, tok_start=dev_i32(start), max_n=50)
+        got.append([qr, out] + [pools[n][i].clone() for n in "kv" for i in ids])
+        del pools, kv
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert bool(torch.isfinite(got[0][1]).all())
