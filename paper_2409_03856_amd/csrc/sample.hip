@@ -535,40 +535,6 @@ __global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) load4<ALIGNED>(row, a.V, v0 + 4 * (tid + j * THREADS), x[j]);
   }
-  if (q.mode == kNone) {  // greedy: the best and its index
-    float best = -INFINITY;
-    int at = INT32_MAX;
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (x[j][e] > best) {
-          best = x[j][e];
-          at = v0 + 4 * (tid + j * THREADS) + e;
-        }
-    for (int o = 1; o < kWave; o <<= 1) {
-      const float ov = __shfl_xor(best, o, kWave);
-      const int oi = __shfl_xor(at, o, kWave);
-      if (ov > best || (ov == best && oi < at)) {
-        best = ov;
-        at = oi;
-      }
-    }
-    if (lane == 0) {
-      s_x[wave] = best;
-      s_i[wave] = at;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < kW; ++w)
-        if (s_x[w] > best || (s_x[w] == best && s_i[w] < at)) {
-          best = s_x[w];
-          at = s_i[w];
-        }
-      a.stat[(size_t)b * a.chunks + c] = ChunkStat{best, best, at, 0, 0, {}, 0};
-    }
-    return;
-  }
   const bool sums = q.mode == kByBins || q.mode == kWhole;  // uniform
   float best = -INFINITY, least = INFINITY;
 #pragma unroll
@@ -608,16 +574,33 @@ __global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
     best = fmaxf(best, s_x[w]);
     least = fminf(least, s_y[w]);
   }
+  if (q.mode == kNone) {  // greedy: the best's first index
+    int at = INT32_MAX;
+#pragma unroll
+    for (int j = PER - 1; j >= 0; --j)
+#pragma unroll
+      for (int e = 3; e >= 0; --e) at = x[j][e] == best ? 4 * j * THREADS + e : at;
+    if (at != INT32_MAX) at += v0 + 4 * tid;
+    for (int o = 1; o < kWave; o <<= 1) at = min(at, __shfl_xor(at, o, kWave));
+    if (lane == 0) s_i[wave] = at;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kW; ++w) at = min(at, s_i[w]);
+      a.stat[(size_t)b * a.chunks + c] = ChunkStat{best, best, at, 0, 0, {}, 0};
+    }
+    return;
+  }
   int finite = min(a.V, v0 + a.chunk) - v0;
   if (const double inv_t = 1.0 / (double)q.temp; sums && far_below(least, (double)best, inv_t, kClear)) {
     // uniform: what weighs something beside the chunk's best, and the least of it; a mask's lowest numbers are not counted
+    const float weighs = logit_of(first_key([&](float y) { return !far_below(y, (double)best, inv_t, kNothing); }));
     float low = INFINITY;
     finite = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (!far_below(x[j][e], (double)best, inv_t, kNothing)) {
+        if (x[j][e] >= weighs) {
           ++finite;
           low = fminf(low, x[j][e]);
         }
@@ -662,13 +645,15 @@ __global__ __launch_bounds__(THREADS) void sample_chunk_kernel(Args a) {
     float reach = bound > key_of(-INFINITY) ? logit_of(bound) : -INFINITY;
     // tokens that weigh nothing stay off the list: few may be left where a mask's lowest numbers are many
     reach = fmaxf(reach, (float)((double)best - (kNothing + 1.0) * (double)q.temp));
+    int from = v0 + 4 * tid;
+    asm volatile("" : "+v"(from));  // or all indices are formed, and held, from the kernel's start on
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (x[j][e] >= reach && x[j][e] > -INFINITY) {
           const int n = atomicAdd(&s_n, 1);
-          if (n < kList) list[n] = (u64)key_of(x[j][e]) << 32 | ~(uint32_t)(v0 + 4 * (tid + j * THREADS) + e);
+          if (n < kList) list[n] = (u64)key_of(x[j][e]) << 32 | ~(uint32_t)(from + 4 * j * THREADS + e);
         }
       }
     __syncthreads();
@@ -885,7 +870,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
         const int c = min(c0 + k * kWaves, a.chunks - 1);
         // a list without a token that reaches the bound is passed over, also one that overflowed
         const int listed = stat[c].listed;
-        n[k] = (c0 + k * kWaves < a.chunks) & (key_of(stat[c].best) >= bound) ? listed : 0;
+        n[k] = ((c0 + k * kWaves < a.chunks) & (key_of(stat[c].best) >= bound)) ? listed : 0;
         if (n[k] > kList) {
           if (lane == 0) atomicAdd(&sh.n, kSort + 1);  // the long way
           n[k] = 0;
