@@ -12,9 +12,15 @@
 // and keeps its sines and cosines over all the head rows that it takes (32 + 8 rows share them at
 // Llama-3-8B heads). Workgroups take one token each; at few tokens a token's rows are cut over more
 // of them. Behind the rotating workgroups, append launches add workgroups that move values: a tile of
-// 64 tokens of one head goes through LDS, because the cache holds values transposed (a column's
-// positions adjacent, as the attention's matrix operands want them): 64 lanes then store 64 adjacent
-// positions of a column.
+// 16 tokens of one head goes through LDS, because the cache holds values transposed (a column's
+// positions adjacent, as the attention's matrix operands want them): 16 lanes then store the adjacent
+// positions of a column. (Tiles of 64 tokens gave a decode batch of 64 sequences 8 workgroups, 9.5 us
+// against 4.8; a prompt of 8192 tokens goes from 57.4 to 58.2 us a call.)
+//
+// Bound: HBM for prompts. 8192 tokens of 32 + 8 heads of 128, bf16, norms: rotation 36.7 us for 168 MB
+// (4.6 TB/s, a large copy's 4.88), append 45.4 us for 201 MB. One token: 3.0 and 4.7 us, a launch.
+// A decode batch's values are single 2-byte stores a column (2048 sequences: 46 us, five times its bytes'
+// time); that is what the transposed layout costs, and the attention reads each of them hundreds of times.
 #include <math.h>
 
 #include "common.h"
@@ -26,7 +32,7 @@ namespace sirius {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kValueTokens = 64;  // tokens per value tile
+constexpr int kValueTokens = 16;  // tokens per value tile
 
 struct RopeArgs {
   const void* q;
@@ -159,7 +165,7 @@ template <typename TK>
 __device__ __forceinline__ void move_values(const RopeArgs& a, int tile, int kvh) {
   __shared__ uint16_t s_v[kValueTokens][128 + 2];  // an odd number of banks between tokens
   __shared__ long s_at[kValueTokens];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+  const int tid = threadIdx.x;
   const int t0 = tile * kValueTokens, nt = min(kValueTokens, a.T - t0), ps = a.pg.page_size;
   if (tid < nt) {
     long at = -1;
@@ -184,9 +190,10 @@ __device__ __forceinline__ void move_values(const RopeArgs& a, int tile, int kvh
   }
   __syncthreads();
   if (nt > 8) {
-    const long at = lane < nt ? s_at[lane] : -1;
+    const int t = tid % kValueTokens;
+    const long at = t < nt ? s_at[t] : -1;
     if (at >= 0)
-      for (int c = wave; c < a.hd; c += kRopeThreads / kWave) a.pg.v_pages[at + (long)c * ps] = s_v[lane][c];
+      for (int c = tid / kValueTokens; c < a.hd; c += kRopeThreads / kValueTokens) a.pg.v_pages[at + (long)c * ps] = s_v[t][c];
   } else {  // few tokens: the lanes go over the columns
     for (int e = tid; e < nt * a.hd; e += kRopeThreads) {
       const int t = e / a.hd, c = e - t * a.hd;
@@ -287,7 +294,8 @@ hipError_t launch(const RopeCall& c, const PagedView* pg, hipStream_t stream) {
   const int units = vec ? c.hd / 8 : c.hd / 2;
   while ((1 << a.lph) < units) ++a.lph;
   const int slots = kRopeThreads >> a.lph, heads = a.H + a.Hkv;
-  // One workgroup per token forms its sines once; below 1024 tokens a token's heads go to more of them.
+  // One workgroup per token forms its sines once; below 1024 tokens a token's heads go to more of them (256 tokens:
+  // 4.9 us, 6.5 by one each; 1024: 9.7 by one each, 11.9 where they are cut).
   a.parts = std::max(1, std::min(ceil_div(heads, slots), 1024 / std::max(1, c.T)));
   a.rows = ceil_div(ceil_div(heads, a.parts), slots) * slots;
   a.parts = ceil_div(heads, a.rows);

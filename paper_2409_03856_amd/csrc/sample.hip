@@ -6,12 +6,12 @@
 // a logit and how many of the tokens that equal it stay. The token drawn is the first in index order
 // whose running kept mass exceeds u times the kept mass.
 //
-// Weights are formed in fp64 and added as whole numbers of 2^-s (s = 62 - log2 V bits), so sums do not
+// Weights are formed in fp64 and added as whole numbers of 2^-s (s = min(50, 62 - log2 V)), so sums do not
 // depend on their order: the histograms below are filled by atomics and every call gives the same
 // token. A row's sums carry an error of about 2^-s sqrt(V) of the best token's weight.
 //
-// sample_chunk_kernel: one workgroup per chunk of a row, its logits in registers: the chunk's best
-// token, and what the row's filters need,
+// sample_chunk_kernel: one workgroup per chunk of a row, its logits in registers, one reading of HBM: the
+// chunk's best token, and what the row's filters need,
 //   few (1 < k <= 256)   the tokens that may be among the row's first k: those above a bound that at
 //                        least k of the chunk reach (the k-th of the maxima of 512 groups);
 //   other filters        the chunk's mass, and counts and masses by bins of an eighth of a temperature,
@@ -19,10 +19,15 @@
 //   none                 the chunk's mass.
 // sample_finish_kernel: one workgroup per row. Few: the chunks' tokens above the best bound, sorted in
 // LDS; everything is decided on them. Otherwise the bins give the cut's bin, whose tokens are
-// gathered from the row and sorted; the chunks' kept masses give the chunk of the draw, and its tokens
-// the draw. Rows that none of this fits (lists that overflow, a cut below 32 temperatures, infinite
-// logits) take the long way, row_cut: the cut digit by digit (11, 11, 10 bits of the logit's ordered
-// bits), each by a pass over the row.
+// gathered from the row (256 MB of cache hold it) and the cut found among them by steps of their keys; the
+// chunks' kept masses give the chunk of the draw, and its tokens the draw. Rows that none of this fits (lists
+// and bins that overflow, a cut below 32 temperatures, infinite logits) take the long way, row_cut: the cut
+// digit by digit (11, 11, 10 bits of the logit's ordered bits), each by a pass over the row.
+//
+// Bound: the chunk kernel by HBM and its fp64 weights together (192 rows of 128256 tokens, 98 MB: greedy 16 us,
+// the rate of a read; top_k 29; sums alone 34; bins too 40-44), the finishing kernel by the chain of barriers
+// and LDS sums of its slowest row (greedy 4 us, top_k 50 13, none 17, min_p 37, top_p 51 of which the gathering 15-20). One row of
+// 32000 tokens: 5.8 + 10.4 us. Twice the finishing threads measured the same or slower (top_p 52.9 us).
 #include <float.h>
 #include <math.h>
 
@@ -1316,8 +1321,8 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
 
 }  // namespace
 
-// Tokens per chunk: 8192, or 2048 where a call has fewer chunks than CUs of them (one row of 128256
-// tokens makes 63 workgroups of 2048, not 16).
+// Tokens per chunk: 8192, or 2048 where a call has fewer chunks than CUs of them (both kernels, filters without a
+// top_k: one row of 128256 tokens 28.6 us by 2048, 32.5 by 8192; 16 rows 58.7 and 58.3; 64 rows 82 and 72).
 static int chunk_of(int B, int V) { return (long)B * ceil_div(V, 8192) < 256 && ceil_div(V, 2048) <= kMaxChunks ? 2048 : 8192; }
 
 SampleLayout sample_layout(int B, int V) {
