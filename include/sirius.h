@@ -528,8 +528,8 @@ typedef struct sirius_paged {
  * A sequence with cache_pos < 0 or tokens behind its table's last row writes nothing, nor does a
  * token whose page is outside [0, n_pages); queries are written all the same. Two tokens must
  * not fall on one row of one page. T == 0 and B == 0 are valid no-ops.
- * Errors: as sirius_rope, plus SIRIUS_EINVAL for the cache's limits above, and T != B max_n without
- * tok_start.
+ * Errors: as sirius_rope, plus SIRIUS_EINVAL for the cache's limits above, T != B max_n without
+ * tok_start, and T n_kv_heads beyond about 2^28.
  */
 int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, const void* v,
                      int kv_dtype, int64_t ldk, int64_t ldv, const sirius_paged* cache,
@@ -592,7 +592,7 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
  * A row without a logit above -infinity, and one with a NaN parameter, a negative or an infinite
  * temperature, gives token -1, kept 0, prob 0. Needs sirius_workspace_size(SIRIUS_OP_SAMPLE, ...).
  * B == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null pointers (where not allowed above), B
- * outside [0, 65535], V outside [1, 2^24], ld outside [V, 2^31], misaligned logits; SIRIUS_EWORKSPACE.
+ * outside [0, 65535], V outside [1, 2^24], B V beyond about 2^37, ld outside [V, 2^31], misaligned logits; SIRIUS_EWORKSPACE.
  */
 int sirius_sample(const float* logits, int64_t ld, int B, int V, const float* u,
                   const float* temperature, const int32_t* top_k, const float* top_p,

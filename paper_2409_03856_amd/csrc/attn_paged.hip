@@ -1086,6 +1086,12 @@ PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf1
   return L;
 }
 
+long paged_attn_grid(const PagedView& pg, int Hkv, const PagedAttnLayout& L) {
+  // every sequence has a unit, and the cuts add fewer than rounds * units
+  const long most = (long)pg.B * ceil_div(pg.max_pages * pg.page_size + kTile, kStep);
+  return (long)Hkv * L.rgroups * (L.units > 1 ? std::min<long>(pg.B + L.rounds * L.units, most) : pg.B);
+}
+
 hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* ws, const PagedAttnLayout& L,
                              hipStream_t stream) {
   Args a{};
@@ -1101,10 +1107,7 @@ hipError_t launch_attn_paged(const PagedAttnCall& c, const PagedView& pg, char* 
   a.po = reinterpret_cast<float*>(ws + L.po);
   const bool mod = c.cap > 0.f || c.slopes != nullptr || c.window > 0 || c.mask != nullptr;
   const int R = a.G * pg.n, rows = group_rows(R, c.q_bf16), ks = ceil_div(c.hd, 32);
-  // every sequence has a unit, and the cuts add fewer than rounds * units
-  const long most = (long)pg.B * ceil_div(pg.max_pages * pg.page_size + kTile, kStep);
-  const long grid = (long)c.Hkv * L.rgroups * (L.units > 1 ? std::min<long>(pg.B + L.rounds * L.units, most) : pg.B);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const long grid = paged_attn_grid(pg, c.Hkv, L);
   {
     ProfScope prof("attn_paged", stream);
     auto launch = [&](auto tq, auto kss, auto mods) {

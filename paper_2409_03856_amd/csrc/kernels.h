@@ -247,12 +247,14 @@ struct RopeCall {
 };
 hipError_t launch_rope(const RopeCall& c, hipStream_t stream);
 hipError_t launch_kv_append(const RopeCall& c, const PagedView& pg, hipStream_t stream);
+long kv_append_grid(int T, int Hkv);  // its workgroups where a token has one for its heads
 
 struct PagedAttnLayout {
   int rgroups, units, rounds;       // query-row groups per kv head, ranges of a round of workgroups, rounds at most
   size_t info, pm, pl, po, total;   // where sequences' partials lie; per unit and row: max, sum, output
 };
 PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16);
+long paged_attn_grid(const PagedView& pg, int Hkv, const PagedAttnLayout& L);  // workgroups of its first kernel
 // q [T][H][hd] (token stride ldq), out [T][H][hd] of the same type; cap 0, slopes null, window 0, mask null: none.
 struct PagedAttnCall {
   const void* q;
@@ -272,6 +274,7 @@ struct SampleLayout {
   size_t stat, list, total;  // what each chunk of a row says of itself; its tokens or bins
 };
 SampleLayout sample_layout(int B, int V);
+long sample_grid(int B, int V);  // workgroups of its first kernel
 // logits [B][V] (row stride ld, 16-byte aligned base); the parameters [B] each, or null.
 struct SampleCall {
   const float* logits;

@@ -314,6 +314,8 @@ hipError_t launch(const RopeCall& c, const PagedView* pg, hipStream_t stream) {
 
 }  // namespace
 
+long kv_append_grid(int T, int Hkv) { return T + (long)ceil_div(T, kValueTokens) * Hkv; }
+
 hipError_t launch_rope(const RopeCall& c, hipStream_t stream) { return launch<false>(c, nullptr, stream); }
 hipError_t launch_kv_append(const RopeCall& c, const PagedView& pg, hipStream_t stream) {
   return launch<true>(c, &pg, stream);

@@ -1335,6 +1335,8 @@ SampleLayout sample_layout(int B, int V) {
   return L;
 }
 
+long sample_grid(int B, int V) { return (long)B * ceil_div(V, chunk_of(B, V)); }
+
 hipError_t launch_sample(const SampleCall& c, char* ws, const SampleLayout& L, hipStream_t stream) {
   Args a{};
   a.logits = c.logits; a.ld = c.ld; a.V = c.V;

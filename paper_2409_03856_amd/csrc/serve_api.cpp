@@ -18,6 +18,7 @@ namespace {
 constexpr int kMaxTokens = 1 << 20;  // tokens per call
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxSeqs = 65535;
+constexpr long kMaxGrid = (1 << 24) - 1;  // workgroups of 256 threads: a launch has fewer than 2^32 threads
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -216,6 +217,7 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
                        (rc = check_ptr(fn, q_out, "q_out"))))
     return rc;
   if ((rc = check_rows(fn, k, "k", Hkv, hd, ldk)) || (rc = check_rows(fn, v, "v", Hkv, hd, ldv))) return rc;
+  if (sirius::kv_append_grid(cache->T, Hkv) > kMaxGrid) return fail(SIRIUS_EINVAL, "%s: T=%d tokens of %d heads are too many", fn, cache->T, Hkv);
   c.q = q; c.k = k; c.v = v;
   c.q_bf16 = q_dtype == SIRIUS_BF16; c.k_bf16 = kv_dtype == SIRIUS_BF16;
   c.ldq = ldq; c.ldk = ldk; c.ldv = ldv;
@@ -245,7 +247,7 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
   const int64_t rows = (int64_t)(H / Hkv) * cache->max_n;
   if (rows > INT32_MAX / 256) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
   const sirius::PagedAttnLayout L = sirius::paged_attn_layout(cache->B, cache->max_n, H, Hkv, hd, q_dtype == SIRIUS_BF16);
-  if ((int64_t)Hkv * L.rgroups * (cache->B + L.rounds * L.units) > INT32_MAX) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
+  if (sirius::paged_attn_grid(view(cache), Hkv, L) > kMaxGrid) return fail(SIRIUS_EINVAL, "%s: too many query rows per call", fn);
   if (ws_bytes < L.total) return fail(SIRIUS_EWORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, L.total);
   sirius::PagedAttnCall c{};
   c.q = q;
@@ -272,6 +274,7 @@ int sirius_sample(const float* logits, int64_t ld, int B, int V, const float* u,
   int rc;
   if ((rc = check_ptr(fn, logits, "logits")) || (rc = check_ptr(fn, ws, "ws"))) return rc;
   if (u == nullptr || token == nullptr) return fail(SIRIUS_EINVAL, "%s: u or token is NULL", fn);
+  if (sirius::sample_grid(B, V) > kMaxGrid) return fail(SIRIUS_EINVAL, "%s: B=%d rows of V=%d are too many", fn, B, V);
   const sirius::SampleLayout L = sirius::sample_layout(B, V);
   if (ws_bytes < L.total) return fail(SIRIUS_EWORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, ws_bytes, L.total);
   const sirius::SampleCall c{logits, (long)ld, B, V, u, temperature, top_k, top_p, min_p, token, kept, prob};

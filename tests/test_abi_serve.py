@@ -163,3 +163,19 @@ def test_sampling_refusals(lib):
         lib.sirius_sample(x, x[:, 0].contiguous())
     with pytest.raises(ValueError, match="fp32"):
         lib.sirius_sample(x.double(), x[:, 0].contiguous())
+
+
+def test_calls_with_more_threads_than_a_launch_holds(lib):
+    """Sizes inside every single limit whose product would pass 2^32 threads are refused, not launched."""
+    L = lib.lib()
+    wide = dict(B=1, T=1 << 20, max_n=1 << 20, n_kv_heads=4096, head_dim=8, max_pages=65536, page_size=16)
+    cache = _paged(lib, **wide)
+    rot = _rotation(lib, rot_dim=8)
+    assert L.sirius_kv_append(None, 0, 0, FAKE, FAKE, 1, 32768, 32768, ctypes.byref(cache), None, 0, ctypes.byref(rot), None, None) == -1
+    assert b"too many" in L.sirius_last_error()
+    cache = _paged(lib, **(wide | dict(B=400, tok_start=1 << 20, n_kv_heads=64)))
+    assert L.sirius_attn_paged(FAKE, 0, 512, ctypes.byref(cache), 64, 0.0, 0.0, None, 0, None, FAKE, FAKE, (1 << 63), None) == -1
+    assert b"too many" in L.sirius_last_error()
+    v = 1 << 24
+    assert L.sirius_sample(FAKE, v, 65535, v, FAKE, None, None, None, None, FAKE, None, None, FAKE, (1 << 63), None) == -1
+    assert b"too many" in L.sirius_last_error()
