@@ -1302,6 +1302,11 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     if (x > -INFINITY && ((u64)key_of(x) << 32 | ~(uint32_t)v) >= cutoff) m += wg.units(wg.weight(x));
   }
   const Scan ts = block_scan(0, m, sh.scan_c, sh.scan_m);
+  if (ts.mt == 0) {  // uniform: tokens that make up units together, none alone (u at 1, a tail far down)
+    __syncthreads();
+    row_cut<ALIGNED>(a, q, wg, b, sh);
+    return;
+  }
   // (the chunk's own sum may be some units off: then its last token of positive mass)
   if (m > 0 && (double)(ts.m - m) <= rest && ((double)ts.m > rest || ts.m == ts.mt)) {
     u64 before = ts.m - m;

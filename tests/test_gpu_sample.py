@@ -182,6 +182,15 @@ def test_cuts_beside_zero_at_hot_temperatures(sr):
             _check(sr, x, u, np.full(5, t, np.float32), np.full(5, k), np.full(5, p, np.float32), np.full(5, m, np.float32))
 
 
+def test_all_of_u_with_a_tail_far_down(sr):
+    """A last chunk whose tokens hold no unit of mass alone but some together: at u = 1 the last token that holds one."""
+    rng = np.random.default_rng(18)
+    x = np.full((1, 24576), -36.0, np.float32)
+    x[:, :2000] = rng.standard_normal((1, 2000))
+    for p in (1.0, 0.9999999):
+        assert _check(sr, x, np.ones(1, np.float32), None, None, np.full(1, p, np.float32), None).tolist() == [1999]
+
+
 def test_rows_beyond_32_bits(sr):
     """Rows so far apart that their offsets pass 2^32 elements; further apart than 2^31 they are refused."""
     import torch
