@@ -26,7 +26,7 @@
 //
 // Bound: the chunk kernel by HBM and its fp64 weights together (192 rows of 128256 tokens, 98 MB: greedy 16 us,
 // the rate of a read; top_k 29; sums alone 34; bins too 40-44), the finishing kernel by the chain of barriers
-// and LDS sums of its slowest row (greedy 4 us, top_k 50 13, none 17, min_p 37, top_p 51 of which the gathering 15-20). One row of
+// and LDS sums of its slowest row (greedy 4 us, top_k 50 11, none 17, min_p 37, top_p 51 of which the gathering 15-20). One row of
 // 32000 tokens: 5.8 + 10.4 us. Twice the finishing threads measured the same or slower (top_p 52.9 us).
 #include <float.h>
 #include <math.h>
@@ -44,7 +44,7 @@ constexpr int kBins = 2048;
 constexpr int kTiles = 4096;      // tiles of a row at most
 constexpr int kTile = 1024;       // tokens per tile, a multiple of this where the row has more tiles
 constexpr int kMaximaAll = 512;   // groups of a chunk whose maxima bound its k-th token
-constexpr int kFew = 256;         // the largest k that goes by lists (192 rows of 128256: k = 250 65 us, 2000 by bins 109)
+constexpr int kFew = 256;         // the largest k that goes by lists (192 rows of 128256: k = 250 62 us, 2000 by bins 109)
 constexpr int kList = 512;        // entries of a chunk's list
 constexpr int kSort = 4096;       // tokens that are sorted in LDS at most
 constexpr int kFine = 256;        // bins of an eighth of a temperature; the last one is never counted
@@ -909,11 +909,21 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
         sh.few_mass[tid] = m;
         sh.few_at[tid] = ~(uint32_t)mine;
       }
+      if (tid < kFew) sh.chunk_mass[tid] = 0;
+      __syncthreads();
+      // each one's mass up to its index, by as many threads as there are for it (50 tokens: 10.6 us, 12.6 by one each)
+      int lp = 6;
+      while (1 << lp < kept.ct) ++lp;
+      if (const int at = tid & ((1 << lp) - 1); at < kept.ct) {
+        const uint32_t here = sh.few_at[at];
+        u64 run = 0;
+        for (int i = tid >> lp; i < kept.ct; i += kThreads >> lp) run += sh.few_at[i] <= here ? sh.few_mass[i] : 0;
+        atomicAdd(&sh.chunk_mass[at], run);
+      }
       __syncthreads();
       if (stays && m > 0) {
         const uint32_t here = sh.few_at[tid];
-        u64 run = 0;  // mass up to this index
-        for (int i = 0; i < kept.ct; ++i) run += sh.few_at[i] <= here ? sh.few_mass[i] : 0;
+        const u64 run = sh.chunk_mass[tid];
         const double target = share_u * (double)kept.mt;
         if ((double)(run - m) <= target && ((double)run > target || run == kept.mt))
           answer((int)here, kept.ct, (float)((double)m / (double)kept.mt));
