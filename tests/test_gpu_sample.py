@@ -182,6 +182,19 @@ def test_cuts_beside_zero_at_hot_temperatures(sr):
             _check(sr, x, u, np.full(5, t, np.float32), np.full(5, k), np.full(5, p, np.float32), np.full(5, m, np.float32))
 
 
+def test_smallest_parameters(sr):
+    """Temperatures, shares and weights at the ends of fp32; u outside [0, 1] counts as its end."""
+    rng = np.random.default_rng(19)
+    x = np.round(_logits(rng, 6, 5000) * 2) / 2
+    x[1] = np.where(rng.random(5000) < 0.01, np.float32(9.5), x[1])
+    x[2] = 0.0
+    u = np.array([-1.0, 0.5, 0.3, 2.0, 1.0, 0.0], np.float32)
+    f = lambda a: np.full(6, a, np.float32)
+    for t, k, p, m in ((1e-40, 0, 1.0, 0.0), (1e-45, 0, 0.9, 0.5), (1e-38, 300, 0.9, 0.0), (1e-40, 7, 1.0, 0.0), (1.0, 0, 1e-40, 0.0),
+                       (1.0, 0, 1.0, 1.0), (1.0, 0, 1.0, 1e-40), (1.0, 5, 1e-45, 1.0), (0.5, 0, 0.99999994, 0.0)):
+        _check(sr, x, u, f(t), np.full(6, k), f(p), f(m))
+
+
 def test_all_of_u_with_a_tail_far_down(sr):
     """A last chunk whose tokens hold no unit of mass alone but some together: at u = 1 the last token that holds one."""
     rng = np.random.default_rng(18)
