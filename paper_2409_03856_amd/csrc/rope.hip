@@ -54,10 +54,6 @@ struct RopeArgs {
 };
 
 __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-__device__ __forceinline__ float value_of(const float* p) { return *p; }
-__device__ __forceinline__ float value_of(const uint16_t* p) { return bf16_lo(*p); }
-__device__ __forceinline__ void put(float* p, float f) { *p = f; }
-__device__ __forceinline__ void put(uint16_t* p, float f) { *p = to_bf16(f); }
 
 template <int VEC>
 __device__ __forceinline__ void load_vec(const float* p, float* x) {

@@ -79,7 +79,6 @@ def _close(got, want):
 def test_prompt_drafts_check_and_sampling(sr):
     """Prompts of three lengths, four drafted tokens one by one, the check's pass over the chunk that rewrites their
     rows, rollback to what each accepts, a sampled token: the positions, the cache and every output follow."""
-    import torch
     s = Step(sr, 3, 80)
     prompts = [17, 1, 30]
     start = np.cumsum([0] + prompts).astype(np.int32)
