@@ -590,7 +590,8 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
  *   token  [B] int32 out; kept [B] int32 out or NULL: how many tokens stayed; prob [B] fp32 out or
  *          NULL: the token's share of the kept mass.
  * A row without a logit above -infinity, and one with a NaN parameter, a negative or an infinite
- * temperature, gives token -1, kept 0, prob 0. Needs sirius_workspace_size(SIRIUS_OP_SAMPLE, ...).
+ * temperature, gives token -1, kept 0, prob 0. Needs sirius_workspace_size(SIRIUS_OP_SAMPLE, ...) for
+ * the call's B and V or any larger ones: the size never falls as either grows.
  * B == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null pointers (where not allowed above), B
  * outside [0, 65535], V outside [1, 2^24], B V beyond about 2^37, ld outside [V, 2^31], misaligned logits; SIRIUS_EWORKSPACE.
  */

@@ -231,7 +231,7 @@ size_t sirius_workspace_size(int op, int B, int d_model, int d_ff, int T_or_V, i
     }
     case SIRIUS_OP_SAMPLE:
       if (B < 0 || B > kMaxLogitRows || T_or_V < 1 || T_or_V > (1 << 24)) return 0;
-      return sirius::sample_layout(std::max(B, 1), T_or_V).total;
+      return sirius::sample_workspace(std::max(B, 1), T_or_V);
     case SIRIUS_OP_TREE_BUILD:
       if (B < 0 || d_model < 1 || d_model > kMaxTreeBuildW || d_ff < 1 || d_ff > kMaxTreeBuildW ||
           T_or_V < 1 || (long)d_model * T_or_V < d_ff)

@@ -274,6 +274,7 @@ struct SampleLayout {
   size_t stat, list, total;  // what each chunk of a row says of itself; its tokens or bins
 };
 SampleLayout sample_layout(int B, int V);
+size_t sample_workspace(int B, int V);  // for every call of at most B rows of at most V tokens
 long sample_grid(int B, int V);  // workgroups of its first kernel
 // logits [B][V] (row stride ld, 16-byte aligned base); the parameters [B] each, or null.
 struct SampleCall {

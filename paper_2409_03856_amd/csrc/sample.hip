@@ -1340,14 +1340,22 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
 // top_k: one row of 128256 tokens 28.6 us by 2048, 32.5 by 8192; 16 rows 58.7 and 58.3; 64 rows 82 and 72).
 static int chunk_of(int B, int V) { return (long)B * ceil_div(V, 8192) < 256 && ceil_div(V, 2048) <= kMaxChunks ? 2048 : 8192; }
 
-SampleLayout sample_layout(int B, int V) {
+static SampleLayout layout_of(size_t chunks) {
   SampleLayout L{};
-  const size_t chunks = (size_t)B * ceil_div(V, chunk_of(B, V));
   Carve c;
   L.stat = c.take(chunks * sizeof(ChunkStat));
   L.list = c.take(chunks * kList * sizeof(u64));
   L.total = c.off;
   return L;
+}
+
+SampleLayout sample_layout(int B, int V) { return layout_of((size_t)B * ceil_div(V, chunk_of(B, V))); }
+
+// What every call of at most B rows of at most V tokens needs. A call has chunks of 2048 only where it has at most 255
+// of 8192, so at most four times as many of them: sizes grow with both arguments, over the border of the rule too.
+size_t sample_workspace(int B, int V) {
+  const size_t large = (size_t)B * ceil_div(V, 8192), small = (size_t)B * ceil_div(V, 2048);
+  return layout_of(std::max(large, std::min<size_t>(small, 4 * 255))).total;
 }
 
 long sample_grid(int B, int V) { return (long)B * ceil_div(V, chunk_of(B, V)); }
