@@ -560,7 +560,8 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
  * probabilities enter the matrix products in pieces that hold every bit. With bf16 queries the
  * probabilities enter with 16 bits, or where H / n_kv_heads * max_n is above 64 rounded to bf16 (as
  * are the terms of the sum that they are divided by).
- * Needs sirius_workspace_size(SIRIUS_OP_ATTN_PAGED, ...) for the call's B and max_n.
+ * Needs sirius_workspace_size(SIRIUS_OP_ATTN_PAGED, ...) for the call's B and max_n or any larger ones: the
+ * size never falls as either grows.
  * T == 0 and B == 0 are valid no-ops. Errors: SIRIUS_EINVAL as sirius_kv_append for q and the
  * cache, H not a multiple of n_kv_heads, scale < 0 or not finite, softcap < 0 or not finite,
  * window < 0, a mask with max_n > 64, too many query rows per call; SIRIUS_EWORKSPACE.

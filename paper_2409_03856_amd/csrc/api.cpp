@@ -226,8 +226,7 @@ size_t sirius_workspace_size(int op, int B, int d_model, int d_ff, int T_or_V, i
       if (B < 0 || d_model < 0 || d_model > kMaxCacheLen || H < 1 || Hkv < 1 || H % Hkv != 0 || T_or_V < 8 ||
           T_or_V > 128 || T_or_V % 8 != 0 || (long)H / Hkv * d_model > INT32_MAX)
         return 0;
-      return std::max(sirius::paged_attn_layout(B, d_model, H, Hkv, T_or_V, false).total,
-                      sirius::paged_attn_layout(B, d_model, H, Hkv, T_or_V, true).total);
+      return sirius::paged_attn_workspace(B, d_model, H, Hkv, T_or_V);
     }
     case SIRIUS_OP_SAMPLE:
       if (B < 0 || B > kMaxLogitRows || T_or_V < 1 || T_or_V > (1 << 24)) return 0;

@@ -1065,25 +1065,44 @@ int group_rows(int rows, bool bf16) { return rows <= kFewRows ? 16 : !bf16 || ro
 
 }  // namespace
 
-PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16) {
-  PagedAttnLayout L{};
-  const int R = H / Hkv * n;
-  L.rgroups = ceil_div(std::max(R, 1), group_rows(R, bf16));
-  const long wgs = (long)Hkv * L.rgroups;
-  // Few rows are bound by memory, which one round and what is over keeps busy; tiles by the matrix units, so
-  // a second round that is not full costs as much as a full one.
-  L.rounds = R <= kFewRows ? 1 : 2;
-  L.units = (int)std::min<long>(std::max((kTargetWgs + (L.rounds == 1 ? wgs - 1 : 0)) / wgs, 1l), kMaxUnits);
-  // A unit is at least the total row count over rounds * units: sequences of more than one unit make fewer
-  // than twice as many of them.
-  const size_t rows = L.units > 1 ? (size_t)2 * L.rounds * L.units * Hkv * R : 0;
+// Where the partials of `rows` (unit, query row)s lie.
+static void place_partials(PagedAttnLayout& L, int B, size_t rows, int hd) {
   Carve c;
   L.info = c.take((size_t)std::max(B, 1) * sizeof(int2));
   L.pm = c.take(rows * sizeof(float));
   L.pl = c.take(rows * sizeof(float));
   L.po = c.take(rows * hd * sizeof(float));
   L.total = c.off;
+}
+static int units_per_round(long wgs, int rounds) {
+  return (int)std::min<long>(std::max((kTargetWgs + (rounds == 1 ? wgs - 1 : 0)) / wgs, 1l), kMaxUnits);
+}
+
+PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16) {
+  PagedAttnLayout L{};
+  const int R = H / Hkv * n;
+  L.rgroups = ceil_div(std::max(R, 1), group_rows(R, bf16));
+  // Few rows are bound by memory, which one round and what is over keeps busy; tiles by the matrix units, so
+  // a second round that is not full costs as much as a full one.
+  L.rounds = R <= kFewRows ? 1 : 2;
+  L.units = units_per_round((long)Hkv * L.rgroups, L.rounds);
+  // A unit is at least the total row count over rounds * units: sequences of more than one unit make fewer
+  // than twice as many of them.
+  place_partials(L, B, L.units > 1 ? (size_t)2 * L.rounds * L.units * Hkv * R : 0, hd);
   return L;
+}
+
+// What every call of at most B sequences and n tokens of each needs, of either type. The partials of one layout do
+// not grow with n: 32 tokens of 32 / 8 heads of 128 take 136 MB, 33 take 70, a long prompt none. Above few rows units *
+// Hkv * rgroups <= kTargetWgs and a group has at most 128 rows, which bounds them all.
+size_t paged_attn_workspace(int B, int n, int H, int Hkv, int hd) {
+  const long R = (long)(H / Hkv) * n;
+  const int units = units_per_round(Hkv, 1);
+  size_t rows = units > 1 ? (size_t)2 * units * Hkv * std::min<long>(R, kFewRows) : 0;
+  if (R > kFewRows && units_per_round(Hkv, 2) > 1) rows = std::max(rows, (size_t)4 * kTargetWgs * std::min(R, 128l));
+  PagedAttnLayout L{};
+  place_partials(L, B, rows, hd);
+  return L.total;
 }
 
 long paged_attn_grid(const PagedView& pg, int Hkv, const PagedAttnLayout& L) {

@@ -254,6 +254,7 @@ struct PagedAttnLayout {
   size_t info, pm, pl, po, total;   // where sequences' partials lie; per unit and row: max, sum, output
 };
 PagedAttnLayout paged_attn_layout(int B, int n, int H, int Hkv, int hd, bool bf16);
+size_t paged_attn_workspace(int B, int n, int H, int Hkv, int hd);  // for every call of at most B sequences and n tokens of each
 long paged_attn_grid(const PagedView& pg, int Hkv, const PagedAttnLayout& L);  // workgroups of its first kernel
 // q [T][H][hd] (token stride ldq), out [T][H][hd] of the same type; cap 0, slopes null, window 0, mask null: none.
 struct PagedAttnCall {

@@ -40,3 +40,30 @@ def test_sampling_workspace_of_the_largest_call_serves_the_smaller_ones(L):
         most = size(b, v)
         for c in ((rng.randint(1, b), v), (b, rng.randint(1, v)), (rng.randint(1, b), rng.randint(1, v))):
             assert need(*c) <= size(*c) <= most, (c, b, v)
+
+
+class PagedC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "cache_pos", "tok_start")] + \
+               [(n, ctypes.c_int) for n in ("B", "T", "max_n", "n_kv_heads", "head_dim", "n_pages", "page_size", "max_pages")]
+
+
+def test_paged_attention_workspace_of_the_largest_call_serves_the_smaller_ones(L):
+    size = lambda b, n, k, g, hd: L.sirius_workspace_size(10, b, n, (k * g << 16) + k, hd, 0)
+
+    def need(b, n, k, g, hd):
+        p = FAKE.value
+        cache = PagedC(p, p, p, p, p, b, b * n, n, k, hd, 9, 16, 4)
+        return max(_needed(L, L.sirius_attn_paged(FAKE, t, k * g * hd, ctypes.byref(cache), k * g, 0.0, 0.0, None, 0, None, FAKE, FAKE, 0,
+                                                  None)) for t in (0, 1))
+
+    for k, g, hd in ((8, 4, 128), (1, 1, 64), (1, 8, 128), (40, 1, 128), (3, 5, 80), (255, 1, 8), (257, 2, 8), (512, 1, 8)):
+        sizes = [size(5, n, k, g, hd) for n in range(0, 1500)]
+        assert sizes == sorted(sizes) and sizes[0] > 0, (k, g, hd)
+        assert all(need(5, n, k, g, hd) <= sizes[n] for n in range(1, 1500)), (k, g, hd)
+    rng = random.Random(6)
+    for _ in range(4000):
+        k, g, hd = rng.randint(1, 64), rng.randint(1, 16), 8 * rng.randint(1, 16)
+        b, n = int(2 ** rng.uniform(0, 10)), int(2 ** rng.uniform(0, 10))
+        most = size(b, n, k, g, hd)
+        for c in ((rng.randint(1, b), n), (b, rng.randint(1, n)), (rng.randint(1, b), rng.randint(1, n))):
+            assert need(*c, k, g, hd) <= size(*c, k, g, hd) <= most, (c, (b, n, k, g, hd))
