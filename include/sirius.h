@@ -558,8 +558,8 @@ int sirius_kv_append(const void* q, int q_dtype, int64_t ldq, const void* k, con
  * pages in front of every token's window are not looked at.
  * Scores, softmax and the weighted sum are fp32 on the stored bf16 keys and values: fp32 queries and
  * probabilities enter the matrix products in pieces that hold every bit. With bf16 queries the
- * probabilities enter with 16 bits, or where H / n_kv_heads * max_n is above 64 rounded to bf16 (as
- * are the terms of the sum that they are divided by).
+ * probabilities enter with 16 bits, or for a sequence with more than 64 rows (H / n_kv_heads times its tokens)
+ * rounded to bf16 (as are the terms of the sum that they are divided by).
  * Needs sirius_workspace_size(SIRIUS_OP_ATTN_PAGED, ...) for the call's B and max_n or any larger ones: the
  * size never falls as either grows.
  * T == 0 and B == 0 are valid no-ops. Errors: SIRIUS_EINVAL as sirius_kv_append for q and the

@@ -719,13 +719,18 @@ constexpr int kRing = 256;  // page entries per half of the ring: 2048 positions
 template <typename TQ, int KS, int QT, bool MOD>
 __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   constexpr bool kF32 = sizeof(TQ) == 4;
-  constexpr int NQ = kF32 ? 3 : 1, NP = kF32 ? 3 : QT == 1 ? 2 : 1;
+  constexpr int NQ = kF32 ? 3 : 1;
+  // Pieces of the probabilities. bf16 ones of a sequence with more than 64 rows go in one, rounded: their output is rounded
+  // to 8 bits too, and two cost a quarter more (prompts of 4500 and 1124 tokens: 213 us with an error of 2.07e-3 of
+  // the output's root mean square, 269 us with 1.64e-3, what the output's own rounding makes). Up to 64 rows, drafted chunks
+  // and single tokens, they keep 16 bits whatever the call's longest sequence is, and the waves share the rows by 16 (48 tokens over up to
+  // 30000 rows in a call for long prompts: 432 us, 438 by one piece, 570 by rows of 32).
+  constexpr bool kByRows = !kF32 && QT == 2;
+  constexpr int kRowsOfTwo = 64;
   // bf16 scores without anything on top: x c - m c in one step, where m starts at a number whose product
   // is finite (a row with scores below it alone goes the long way)
   constexpr bool kFused = !kF32 && !MOD;
   constexpr float kFusedMin = -1e30f;
-  // One rounded piece: the sum is of the rounded probabilities, by a product with ones.
-  constexpr bool kOnes = NP == 1;
   constexpr int DT = KS * 2, kC = KS == 2 ? 8 : 16;  // 16-byte chunks of a key row in LDS
   constexpr int kKLoads = kTileP * kC / kThreads, kVLoads = KS * 32 * 8 / kThreads;
   constexpr int kKChunks = kTileP * kC, kVChunks = KS * 32 * 8;
@@ -753,15 +758,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   const int c1 = min(u.c1, last + 1);
   int c0 = u.c0;
   if (MOD && a.window > 0) c0 = max(c0, (u.p + r0 / a.G + 1 - a.window) & ~(kTile - 1));
-  const int w0 = r0 + 16 * QT * wave;  // this wave's rows
+  const bool few = kByRows && nrows <= kRowsOfTwo;  // uniform
+  const int tiles = few ? 1 : QT;                   // of 16 rows, this wave's
+  const int w0 = r0 + 16 * tiles * wave;
   bf16x8_t qf[QT][KS][NQ];
   RowLimits lim[QT];
   float slope[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = w0 + 16 * t + fr, i = r / a.G, h = kvh * a.G + (r - i * a.G);
-    const bool there = r < nrows;
-    lim[t] = limits<MOD>(a, u, r, nrows);
+    const bool there = r < nrows && t < tiles;
+    lim[t] = limits<MOD>(a, u, r, there ? nrows : 0);
     slope[t] = MOD && a.slopes != nullptr && there ? a.slopes[h] : 0.f;
     load_query<TQ, KS, NQ>(static_cast<const TQ*>(a.q) + (long)(u.first + (there ? i : 0)) * a.ldq + (long)(there ? h : 0) * a.hd,
                            there, g, hd8, qf[t]);
@@ -778,7 +785,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   }
   const float to_exp2 = a.scale * 1.44269504088896341f, inv_cap = MOD && a.cap > 0.f ? 1.f / a.cap : 0.f;
   const float slack = kF32 || MOD ? 4.f : 4.f / a.scale;
-  const int wlast = w0 < nrows ? u.p + (min(w0 + 16 * QT, nrows) - 1) / a.G : -1;  // the last row this wave sees
+  const int wlast = w0 < nrows ? u.p + (min(w0 + 16 * tiles, nrows) - 1) / a.G : -1;  // the last row this wave sees
   const int low_last = MOD && a.window > 0 ? max(0, wlast + 1 - a.window) : 0;
   if (tid == 0) s_bad = 0;
   __syncthreads();
@@ -846,36 +853,38 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < kVLoads; ++j) buf[v_at(vr + j * (kThreads / 8), vc)] = vw[j];
   };
-  auto compute = [&](const uint4* buf, int t0) {
+  auto compute = [&](auto np, auto qt, const uint4* buf, int t0) {
+    constexpr int NP = decltype(np)::value, QN = decltype(qt)::value;
+    constexpr bool kOnes = NP == 1;  // one rounded piece: the sum is of the rounded probabilities, by a product with ones
     if (t0 > wlast) return;  // uniform over the wave
     const bf16x8_t* frag = reinterpret_cast<const bf16x8_t*>(buf);
-    float x[QT][2][8];  // positions t0 + 32 nb + 8 g + e
+    float x[QN][2][8];  // positions t0 + 32 nb + 8 g + e
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        floatx4_t hi[QT], low[QT];
+        floatx4_t hi[QN], low[QN];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) hi[t] = low[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < QN; ++t) hi[t] = low[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           const bf16x8_t kf = frag[k_at(32 * nb + 8 * (fr >> 2) + 4 * h + (fr & 3), 4 * s + g)];
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
+          for (int t = 0; t < QN; ++t) {
 #pragma unroll
             for (int pc = NQ - 1; pc > 0; --pc) low[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][pc], low[t], 0, 0, 0);
             hi[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][s][0], hi[t], 0, 0, 0);
           }
         }
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QN; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[t][nb][4 * h + e] = kF32 ? hi[t][e] + low[t][e] : hi[t][e];
       }
     // some row of the wave does not see all of it (a mask may hide row p from its own token)
     const bool part = t0 + kTileP > min(c1, MOD && a.mask != nullptr ? u.p : u.p + w0 / a.G + 1);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
+    for (int t = 0; t < QN; ++t) {
       modify<MOD, kF32, 16>(a, &x[t][0][0], lim[t], slope[t], inv_cap, t0, g);
       if (part || (MOD && t0 < low_last)) {  // uniform over the wave
         asm volatile("");  // a branch, not 48 instructions of every tile
@@ -900,8 +909,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
         const float m_new = __builtin_elementwise_maximum(m[t], mx);
         const float alpha = kF32 ? exp_neg(m[t] - m_new) : __builtin_amdgcn_exp2f((m[t] - m_new) * c);
         m[t] = m_new;
-        l[t] *= alpha;
-        ls[t] *= alpha;
+        if constexpr (kOnes) ls[t] *= alpha;
+        else l[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
       }
@@ -915,29 +924,29 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
           y = kF32 ? exp_neg(y - m[t]) : __builtin_amdgcn_exp2f(kFused ? fmaf(y, c, -mc) : (y - m[t]) * c);
           if (!kOnes) sum += y;
         }
-      l[t] += sum;
+      if (!kOnes) l[t] += sum;
     }
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb) {
-      bf16x8_t pf[QT][NP];
+      bf16x8_t pf[QN][NP];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) pieces<NP>(x[t][nb], pf[t]);
+      for (int t = 0; t < QN; ++t) pieces<NP>(x[t][nb], pf[t]);
       if constexpr (kOnes) {
         const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
 #pragma unroll
-        for (int t = 0; t < QT; ++t) ls[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t][0], ls[t], 0, 0, 0);
+        for (int t = 0; t < QN; ++t) ls[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t][0], ls[t], 0, 0, 0);
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const bf16x8_t vf = frag[v_at(16 * d + fr, 4 * nb + g)];
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QN; ++t)
 #pragma unroll
           for (int pc = NP - 1; pc >= 0; --pc) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t][pc], o[t][d], 0, 0, 0);
       }
     }
   };
-  if (c0 < c1) {
+  auto walk = [&](auto np, auto qt) {
     stage(0);
     __syncthreads();
     load(c0);
@@ -947,8 +956,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
       if (i % (kRing * 8 / kTileP) == 0) stage(++seg);  // read from the last tile of this half on
       __syncthreads();
       if (t0 + kTileP < c1) load(t0 + kTileP);
-      compute(s_kv[i & 1], t0);
+      compute(np, qt, s_kv[i & 1], t0);
       if (t0 + kTileP < c1) store(s_kv[(i + 1) & 1], t0 + kTileP);
+    }
+  };
+  if (c0 < c1) {
+    using std::integral_constant;
+    if constexpr (kByRows) {
+      if (few) walk(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+      else walk(integral_constant<int, 1>{}, integral_constant<int, QT>{});
+    } else {
+      walk(integral_constant<int, kF32 ? 3 : 2>{}, integral_constant<int, QT>{});
     }
   }
   __syncthreads();
@@ -961,7 +979,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
   for (int t = 0; t < QT; ++t) {
     l[t] += __shfl_xor(l[t], 16, kWave);
     l[t] += __shfl_xor(l[t], 32, kWave);
-    if (kOnes) l[t] = ls[t][0];
+    if (kByRows) l[t] += ls[t][0];  // one of them is 0
     if (kFused) odd |= !(l[t] > 0.f) && lim[t].last >= c0;
     floatx4_t chk = floatx4_t{l[t], 0.f, 0.f, 0.f};
 #pragma unroll
@@ -972,14 +990,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_tiles_kernel(Args a) {
     Unit w = u;
     w.c0 = c0;
     w.c1 = c1;
-    for (int r = w0; r < min(w0 + 16 * QT, nrows); ++r)
+    for (int r = w0; r < min(w0 + 16 * tiles, nrows); ++r)
       whole_row<TQ>(a, w, r, kvh, u.count > 1 ? a.po + (prow + r) * a.hd : nullptr, a.pm + prow + r, a.pl + prow + r);
     return;
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = w0 + 16 * t + fr;
-    if (r >= nrows) continue;
+    if (r >= nrows || t >= tiles) continue;
     const float unit = kF32 || MOD ? 1.f : a.scale;
     if (u.count > 1) {
       if (g == 0) {

@@ -1,0 +1,66 @@
+"""GPU parity of calls over the paged cache whose outcome must not follow from other sequences of the call or from arguments that
+say nothing of the data, against the 64-bit oracle.
+
+Tolerances, relative to the root mean square of the oracle's output. bf16 queries: half a step of the output, 2^-8
+of its value; probabilities cut to 16 bits are 2^-15 of themselves off at most, scores' fp32 roundings below 60 2^-24 of
+|q| |k| / sqrt(hd): 0.002 together with values of up to 5 times the root mean square, as in the other tests of this entry
+point. Probabilities rounded to bf16 do not meet it: 2^-9 each, a thousandth of the root mean square at a deviation of one
+for sums that a few rows carry, thrice that among ten thousand outputs.
+"""
+
+import numpy as np
+import pytest
+
+import oracle
+from oracle import serve
+from synth import bf16_bits
+from gpu_util import say, dev_bf16, dev_f32, dev_i32, host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sr():
+    import paper_2409_03856_amd as sr
+    sr.lib()
+    return sr
+
+
+def _inputs(seed, before, new, page, h, hkv, hd):
+    rng = np.random.default_rng(seed)
+    need = [-(-(p + n) // page) for p, n in zip(before, new)]
+    pages = sum(need) + 1
+    order = rng.permutation(pages)
+    table = np.full((len(before), max(need)), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    q = bf16_bits(rng.standard_normal((sum(new), h, hd)).astype(np.float32))
+    kp = bf16_bits(rng.standard_normal((pages, hkv, page, hd)).astype(np.float32))
+    vp = bf16_bits(rng.standard_normal((pages, hkv, hd, page)).astype(np.float32))
+    return rng, q, kp, vp, table, np.cumsum([0] + list(new)).astype(np.int32)
+
+
+def _call(sr, q, kp, vp, table, before, start, **kw):
+    out = sr.sirius_attn_paged(dev_bf16(q), dev_bf16(kp), dev_bf16(vp), dev_i32(table), dev_i32(np.array(before)),
+                               tok_start=dev_i32(start), **kw)
+    return oracle.widen_bf16(host(out)).astype(np.float64)
+
+
+@pytest.mark.parametrize("h,hkv,hd", [(32, 8, 128), (12, 4, 96), (8, 2, 64)])
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=30.0), dict(window=150)])
+def test_few_rows_keep_their_precision_whatever_the_call(sr, h, hkv, hd, kw):
+    """Decoded tokens and short chunks beside a prompt, and without max_n, have 16 bits of their probabilities."""
+    rng, q, kp, vp, table, start = _inputs(hd, [60, 7, 200, 300, 0, 33], [1, 5, 1, 3, 140, 1], 16, h, hkv, hd)
+    before = [60, 7, 200, 300, 0, 33]
+    want = serve.attn_paged(oracle.widen_bf16(q), kp, vp, table, before, start, **kw)
+    got = _call(sr, q, kp, vp, table, before, start, **kw)
+    few = np.r_[0:10, 150]  # every sequence but the prompt
+    rms = float(np.sqrt(np.mean(want[few] ** 2)))
+    err = float(np.max(np.abs(got[few] - want[few]) - 2.0 ** -8 * np.abs(want[few]))) / rms
+    say(f"  H={h}/{hkv} hd={hd} {kw}: {err:.2e} x RMS beyond the output's rounding")
+    assert err <= 0.002
+    many = slice(10, 150)
+    more = 2.0 ** -8 * (serve.attn_paged(oracle.widen_bf16(q), kp, vp & 0x7fff, table, before, start, **kw)[many] + 2 * np.abs(want[many]))
+    assert (np.abs(got[many] - want[many]) <= more + 0.002 * float(np.sqrt(np.mean(want[many] ** 2)))).all()
