@@ -669,9 +669,9 @@ def sirius_rope(q, k, positions, freqs, *, interleaved=False, mscale=1.0, norm_e
     return q_out, k_out
 
 
-def _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n):
-    """The call's sirius_paged as bytes, for T tokens of head size hd, and its B, max_n and number of heads (max_n None: T, or
-    T / B without tok_start)."""
+def _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n, most=1 << 20):
+    """The call's sirius_paged as bytes, for T tokens of head size hd, and its B, max_n and number of heads (max_n None: T / B
+    without tok_start; with it T, or the rows of a table or `most` where those are fewer: no sequence may have more)."""
     pages, hkv, size, d = k_pages.shape
     if k_pages.dtype is not names.bf16 or v_pages.dtype is not names.bf16 or not k_pages.is_contiguous() or not v_pages.is_contiguous():
         raise ValueError("k_pages and v_pages must be contiguous bf16 [pages, ...]")
@@ -685,7 +685,7 @@ def _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max
     if tok_start is not None:
         _vector(tok_start, names.i32, bsz + 1, "tok_start")
         start = tok_start.data_ptr()
-        n = t if max_n is None else int(max_n)
+        n = min(t, wide * size, most) if max_n is None else int(max_n)
     else:
         _need(bsz == 0 or t % bsz == 0, "without tok_start every sequence has T / B tokens")
         n = t // bsz if bsz else 0
@@ -747,8 +747,9 @@ def sirius_attn_paged(q, k_pages, v_pages, page_table, cache_pos, *, tok_start=N
                       slopes=None, window=0, mask=None, out=None, ws=None, stream=None):
     """q [T, H, hd] (fp32 or bf16, tokens may be apart) over the cache that sirius_kv_append fills, after the
     append and before cache_pos moves. tok_start [B + 1] int32 or None (T / B tokens each); max_n: the most
-    tokens of a sequence (with tok_start, T unless given). slopes [H] fp32, mask [T] int64 words of chunk
-    bits. Returns out [T, H, hd] of q's type."""
+    tokens of a sequence, from which the kernel and the cut of the work are chosen (with tok_start T unless given, 64
+    with a mask: give it where sequences have fewer, a batch of decoded tokens takes a sixth less with max_n=1). slopes
+    [H] fp32, mask [T] int64 words of chunk bits. Returns out [T, H, hd] of q's type."""
     if stream is not None:
         return _on(stream, sirius_attn_paged, locals())
     names = _names or _bound()
@@ -772,7 +773,8 @@ def sirius_attn_paged(q, k_pages, v_pages, page_table, cache_pos, *, tok_start=N
         _vector(mask, names.i64, t, "mask")
         bits = mask.data_ptr()
     _four(k_pages, "k_pages")
-    cache, bsz, n, hkv = _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n)
+    cache, bsz, n, hkv = _paged(names, t, hd, k_pages, v_pages, page_table, cache_pos, tok_start, max_n,
+                                1 << 20 if mask is None else 64)
     if ws is None:
         ws = workspace(OP_ATTN_PAGED, bsz, n, h * 65536 + hkv, hd, device=q.device)
     rc = (_lib or lib()).sirius_attn_paged(q.data_ptr(), qt, ldq, cache, h, scale, softcap, sl, window, bits, out.data_ptr(),

@@ -64,3 +64,42 @@ def test_few_rows_keep_their_precision_whatever_the_call(sr, h, hkv, hd, kw):
     many = slice(10, 150)
     more = 2.0 ** -8 * (serve.attn_paged(oracle.widen_bf16(q), kp, vp & 0x7fff, table, before, start, **kw)[many] + 2 * np.abs(want[many]))
     assert (np.abs(got[many] - want[many]) <= more + 0.002 * float(np.sqrt(np.mean(want[many] ** 2)))).all()
+
+
+def test_masked_trees_without_max_n(sr):
+    """A batch of trees with more than 64 nodes in all: each has fewer, so their masks hold."""
+    import torch
+    before, new = [30, 0, 100, 5, 61], [16, 20, 16, 13, 64]
+    rng, q, kp, vp, table, start = _inputs(21, before, new, 8, 8, 2, 64)
+    mask = []
+    for n in new:
+        bits = []
+        for i in range(n):
+            bits.append((bits[rng.integers(i)] if i and rng.random() < 0.8 else 0) | 1 << i)
+        mask += bits
+    words = torch.from_numpy(np.array(mask, np.uint64).view(np.int64)).cuda()
+    want = serve.attn_paged(oracle.widen_bf16(q), kp, vp, table, before, start, mask=mask)
+    got = _call(sr, q, kp, vp, table, before, start, mask=words)
+    rms = float(np.sqrt(np.mean(want ** 2)))
+    more = 2.0 ** -8 * (np.abs(want) + serve.attn_paged(oracle.widen_bf16(q), kp, vp & 0x7fff, table, before, start, mask=mask))
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + more + 0.002 * rms).all()
+    given = _call(sr, q, kp, vp, table, before, start, mask=words, max_n=64)
+    assert np.array_equal(got, given)
+    # 65 tokens of one sequence have no bits: NaN, the others as they are
+    got = _call(sr, q, kp, vp, np.ascontiguousarray(table[:3]), [30, 0, 0], np.array([0, 16, 36, 36 + 65], np.int32), mask=words)
+    assert np.isnan(got[36:101]).all() and np.isfinite(got[:36]).all()
+
+
+def test_max_n_left_out_is_what_a_table_holds(sr):
+    """Short tables: the call is made for their rows, and a sequence beyond them gets NaN with and without max_n."""
+    before, new = [0, 3, 9], [6, 1, 5]
+    rng, q, kp, vp, table, start = _inputs(22, before, new, 8, 4, 2, 64)
+    short = np.ascontiguousarray(table[:, :1])
+    start2 = np.array([0, 6, 7, 12], np.int32)
+    a = _call(sr, q, kp, vp, short, before, start2)
+    b = _call(sr, q, kp, vp, short, before, start2, max_n=12)
+    assert np.isnan(a[7:]).all() and np.array_equal(a[7:], b[7:], equal_nan=True)
+    want = serve.attn_paged(oracle.widen_bf16(q), kp, vp, short, before, start2)
+    rms = float(np.sqrt(np.mean(want[:7] ** 2)))
+    for got in (a, b):
+        assert (np.abs(got[:7] - want[:7]) <= 2.0 ** -8 * np.abs(want[:7]) + 0.002 * rms).all()
