@@ -47,8 +47,9 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kTile = 32;           // positions per wave step
-constexpr int kStep = kTile * kWaves;
+constexpr int kTile = kPlanTile;    // positions per wave step
+constexpr int kStep = kPlanStep;
+static_assert(kStep == kTile * kWaves, "a step is a tile of each wave");
 constexpr int kTargetWgs = 512;     // workgroups wanted: two per CU, what their registers allow
 constexpr int kMaxUnits = 256;      // units of a round at most
 constexpr int kGroups = 512;        // 8-position groups whose pages are staged at a time
@@ -126,8 +127,6 @@ __device__ __forceinline__ int wave_add(int v) {
   return v;
 }
 
-__device__ __forceinline__ int whole_steps(long rows) { return (int)((max(rows, 1l) + kStep - 1) / kStep * kStep); }
-
 // How the call's sequences are cut. Every workgroup counts for itself, one sequence per lane.
 struct Plan {
   int every;          // rows per unit at most
@@ -176,7 +175,7 @@ __device__ __forceinline__ Plan make_plan(const Args& a) {
     int most = p.span;
     for (int m = 1; m < kWave; m <<= 1) most = max(most, __shfl_xor(most, m, kWave));
     const int half = whole_steps((total + 2 * a.units - 1) / (2 * a.units));
-    const int one = wave_add((p.span + p.every - 1) / p.every), two = wave_add((p.span + half - 1) / half);
+    const int one = wave_add(units_of(p.span, p.every)), two = wave_add(units_of(p.span, half));
     auto cost = [&](int units, int rows) { return (units + a.units - 1) / a.units * (rows + kOvh); };
     int best = cost(one, p.every);
     if (cost(two, half) < best) {
@@ -186,7 +185,7 @@ __device__ __forceinline__ Plan make_plan(const Args& a) {
     const int fit = B <= a.units ? whole_steps((most + a.units / B - 1) / (a.units / B)) : INT32_MAX / 2;
     if (fit + kOvh < best) p.every = fit;
   }
-  p.cnt = (p.span + p.every - 1) / p.every;
+  p.cnt = units_of(p.span, p.every);
   p.ic = p.cnt;
   p.is = p.cnt > 1 ? p.cnt : 0;
   scan2(lane, p.ic, p.is);
@@ -221,7 +220,7 @@ __device__ __forceinline__ Unit unit_at(const Args& a, const Plan& p, int number
     if (tid == 0) s_hit[0] = -1;
     for (int b0 = 0; b0 < B; b0 += kThreads) {
       const int s = b0 + tid < B ? span_of(a, b0 + tid) : 0;
-      const int cnt = (s + p.every - 1) / p.every, sl = cnt > 1 ? cnt : 0;
+      const int cnt = units_of(s, p.every), sl = cnt > 1 ? cnt : 0;
       int ic = cnt, is = sl;
       scan2(lane, ic, is);
       if (lane == kWave - 1) {

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "paged_plan.h"
 
 namespace sirius {
 
@@ -21,7 +22,6 @@ struct PagedView {
 };
 
 constexpr int kMaxPageSize = 4096;     // row * (magic * page_size - 2^32) < 2^20 * 2^12 stays below 2^32
-constexpr int kMaxPagedRows = 1 << 20;  // max_pages * page_size
 
 __device__ __forceinline__ int page_of(const PagedView& c, int row) {
   return (int)__umulhi((uint32_t)row, c.page_magic);
