@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -255,7 +256,7 @@ int sirius_attn_paged(const void* q, int q_dtype, int64_t ldq, const sirius_page
   c.ldq = ldq;
   c.H = H; c.Hkv = Hkv; c.hd = hd;
   c.scale = scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)hd));
-  c.cap = softcap;
+  c.cap = softcap > 0.f ? std::max(softcap, FLT_MIN) : 0.f;  // 1 / cap stays finite (a score of 0 times it, 0)
   c.slopes = slopes;
   c.window = window;
   c.mask = mask;

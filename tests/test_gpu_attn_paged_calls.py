@@ -103,3 +103,17 @@ def test_max_n_left_out_is_what_a_table_holds(sr):
     rms = float(np.sqrt(np.mean(want[:7] ** 2)))
     for got in (a, b):
         assert (np.abs(got[:7] - want[:7]) <= 2.0 ** -8 * np.abs(want[:7]) + 0.002 * rms).all()
+
+
+@pytest.mark.parametrize("cap", [1e-45, 1e-39, 2.0 ** -127, 1.2e-38, 3e38])
+def test_caps_at_the_ends_of_fp32(sr, cap):
+    """The smallest caps leave every row the same score, the largest leave scores as they are; one token and a prompt."""
+    for before, new in (([70, 3], [1, 1]), ([5], [80])):
+        rng, q, kp, vp, table, start = _inputs(23, before, new, 16, 4, 2, 64)
+        kp[table[0, 0], :, 2] = 0  # a score of 0
+        want = serve.attn_paged(oracle.widen_bf16(q), kp, vp, table, before, start, softcap=float(np.float32(cap)))
+        got = _call(sr, q, kp, vp, table, before, start, softcap=cap)
+        rms = float(np.sqrt(np.mean(want ** 2)))
+        more = 2.0 ** -8 * (np.abs(want) + serve.attn_paged(oracle.widen_bf16(q), kp, vp & 0x7fff, table, before, start,
+                                                            softcap=float(np.float32(cap)))) if new == [80] else 0.0
+        assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + more + 0.002 * rms).all(), (cap, new)
