@@ -8,7 +8,8 @@
 //
 // Weights are formed in fp64 and added as whole numbers of 2^-s (s = min(50, 62 - log2 V)), so sums do not
 // depend on their order: the histograms below are filled by atomics and every call gives the same
-// token. A row's sums carry an error of about 2^-s sqrt(V) of the best token's weight.
+// token. A row's sums are off by about 2^-s sqrt(V) of the best token's weight, by V / 2 2^-s at most (a tail of equal
+// weights just beside half a unit).
 //
 // sample_chunk_kernel: one workgroup per chunk of a row, its logits in registers, one reading of HBM: the
 // chunk's best token, and what the row's filters need,
