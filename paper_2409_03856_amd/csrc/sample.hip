@@ -1305,7 +1305,7 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
   __syncthreads();
   // ---- its tokens, the same number to each thread
   const int c = sh.bin, each = a.chunk / kThreads, first = c * a.chunk + tid * each;
-  const double rest = target - (double)sh.bm;
+  const double share = (target - (double)sh.bm) / (double)sh.chunk_mass[c];  // of its kept mass
   u64 m = 0;
   for (int e = 0; e < each; ++e) {
     const int v = first + e;
@@ -1318,7 +1318,9 @@ __global__ __launch_bounds__(kThreads) void sample_finish_kernel(Args a) {
     row_cut<ALIGNED>(a, q, wg, b, sh);
     return;
   }
-  // (the chunk's own sum may be some units off: then its last token of positive mass)
+  // The chunk's own sum may be off its mass in the row's units (tokens of half a unit count as one each here): the same
+  // share of it, and at u = 1, whatever these quotients round to, the last token of positive mass.
+  const double rest = share_u < 1.0 ? share * (double)ts.mt : INFINITY;
   if (m > 0 && (double)(ts.m - m) <= rest && ((double)ts.m > rest || ts.m == ts.mt)) {
     u64 before = ts.m - m;
     for (int e = 0; e < each; ++e) {

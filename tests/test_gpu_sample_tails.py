@@ -43,3 +43,23 @@ def test_tails_beside_half_a_unit(sr, v, beside, k, p):
         share = 1.0 / (1.0 + (want[1] - 1) * math.exp(float(x[b].min()))) if x[b, tok[b]] == 0.0 else 0.0
         assert abs(prob[b] - share) <= 2.0 ** -24 * share + 2 * off, (b, prob[b], share)
     say(f"  V={v} s={s} {beside} of half a unit, k={k} p={p}: tokens {tok.tolist()}")
+
+
+@pytest.mark.parametrize("v", [9000, 128256, 1 << 21])
+def test_the_last_token_of_positive_mass_at_one(sr, v):
+    """A chunk's tokens of half a unit and more count as one each, so that they sum to more than the chunk's share of the
+    row: u = 1 draws the last of them all the same, with every filter that leaves it."""
+    s = min(50, 62 - math.ceil(math.log2(v)))
+    x = np.full((3, v), math.log(1.01 * 2.0 ** -(s + 1)), np.float32)
+    x[0, 0] = x[1, v // 2] = x[2, 7] = 0.0
+    x[2, v - 100:] = -np.inf
+    u = dev_f32(np.ones(3))
+    for kw in (dict(), dict(min_p=1e-30), dict(top_k=v - 200), dict(temperature=0.999)):
+        tok, kept, _ = (host(t).tolist() for t in sr.sirius_sample(dev_f32(x), u, **kw))
+        if "temperature" in kw:  # each below half a unit then: the best one alone has mass
+            assert tok == [0, v // 2, 7], (kw, tok)
+        elif "top_k" in kw:  # the first of the tied ones stay
+            assert tok == [v - 201] * 3, (kw, tok)
+            assert kept == [v - 200] * 3
+        else:
+            assert tok == [v - 1, v - 1, v - 101], (kw, tok)
