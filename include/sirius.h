@@ -483,8 +483,8 @@ int sirius_rope_freqs(double* freqs, int rot_dim, double theta, int scaling, dou
  *         k is bf16 and ldk = Hkv head_dim.
  * T == 0 is a valid no-op. Errors: SIRIUS_EINVAL for null or misaligned (16 bytes) pointers, an
  * unknown dtype, head_dim not a multiple of 8 in [8, 128], H or Hkv outside [1, 4096], T outside
- * [0, 2^20], a bad stride, and a bad rotation (rot_dim odd or outside [0, head_dim], mscale not
- * finite, norm_eps NaN).
+ * [0, 2^20], a bad stride, and a bad rotation (rot_dim odd or outside [0, head_dim], mscale or
+ * norm_eps not finite, freqs or a weight not 16-byte aligned).
  */
 int sirius_rope(const void* q, int q_dtype, int64_t ldq, const void* k, int k_dtype, int64_t ldk,
                 const int32_t* positions, int T, int H, int Hkv, int head_dim,
@@ -501,7 +501,9 @@ int sirius_rope(const void* q, int q_dtype, int64_t ldq, const void* k, int k_dt
  *   page_table [B, max_pages] int32; pages may be shared by sequences that only read them
  *   cache_pos  [B] int32
  *   tok_start  [B + 1] int32, ascending from 0, or NULL: max_n tokens each, T = B max_n.
- *   max_n      at least the longest sequence's tokens in this call.
+ *   max_n      at least the longest sequence's tokens in this call. Attention chooses its kernel and cuts its work for
+ *              that many of every sequence: a close bound is faster, and prompts beside decoded tokens are two calls
+ *              better than one.
  * All pointers are device pointers. Tokens at or behind tok_start[B] belong to no sequence: their
  * outputs are left as they were. Limits: page_size a multiple of 8 in [8, 4096], max_pages *
  * page_size <= 2^20, head_dim a multiple of 8 in [8, 128], B <= 65535, T <= 2^20.

@@ -799,8 +799,8 @@ def _per_row(v, dtype, bsz, device, name):
 def sirius_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, token=None, kept=None, prob=None,
                   ws=None, stream=None):
     """logits [B, V] fp32 (rows may be apart), u [B] fp32 in [0, 1). temperature, top_p, min_p: fp32 [B]
-    or one number, top_k: int32 [B] or one number, None: off (temperature 1). Returns (token [B] int32, kept
-    [B] int32, prob [B] fp32)."""
+    or one number (filled into a tensor by a launch of its own), top_k: int32 [B] or one number, None: off
+    (temperature 1). Returns (token [B] int32, kept [B] int32, prob [B] fp32)."""
     if stream is not None:
         return _on(stream, sirius_sample, locals())
     names = _names or _bound()

@@ -14,8 +14,9 @@
 // 32 positions each and are merged at the end. Scores are K Q^T on the matrix units, whose result (a lane
 // holds one query row and, by the order in which key rows are dealt to the operand's rows, eight
 // consecutive positions) is the operand of V^T P^T as it is. Keys lie row by row and values column by
-// column in the cache, so that both operands are 16-byte loads straight into registers: no LDS, no
-// barrier in the loop, one tile ahead in flight. fp32 queries and their probabilities go in as three
+// column in the cache, so that both operands are 16-byte loads straight into registers, one tile ahead in
+// flight: LDS holds the page entries of 4096 positions, staged behind a barrier, and the pieces of fp32 queries, and
+// no tile waits for another wave. fp32 queries and their probabilities go in as three
 // bf16 pieces that hold every bit; bf16 ones in one piece and probabilities in two.
 // Bound: HBM. 48 sequences of up to 30000 rows, 32 / 8 heads of 128, bf16: 350 us for 1.85 GB of keys and values,
 // 5.3 TB/s (a plain read's rate here); fp32 queries 365 us. One token over 2048 rows: 9.8 us, a chain of launch,
@@ -23,10 +24,13 @@
 //
 // attn_tiles_kernel: more rows, in tiles of LDS that four waves share (below).
 // Bound: the matrix units and the vector instructions between their products, which two waves of a SIMD only
-// partly overlap. Prompts of 4500 and 1124 tokens, bf16: 199 us, 880 TFLOP/s (a large library product reaches
-// 1140 to 1360), matrix units busy 41 % at the clock that a counter run keeps; eight trees of 40 nodes over 6000
+// partly overlap. Prompts of 4500 and 1124 tokens, bf16: 206 us, 855 TFLOP/s (a large library product reaches
+// 1140 to 1360), matrix units busy 41 % at the clock that a counter run keeps; the same with fp32 queries, three products
+// for one, 590 us, 299 TFLOP/s; eight trees of 40 nodes over 6000
 // rows, fp32, capped: 155 us and the merge 9, matrix units busy 25 % (six products a tile, then 48 exponentials' and
-// pieces' instructions a lane).
+// pieces' instructions a lane). Row groups and cuts are made for max_n tokens of every sequence: beside a long prompt a
+// decoded token is one workgroup's per head, from its first row to its last (a prompt of 4096 tokens and 32 tokens over up to
+// 30000 rows, bf16: 1086 us in one call, 178 and 293 in two).
 #include <float.h>
 #include <math.h>
 

@@ -18,7 +18,7 @@
 // against 4.8; a prompt of 8192 tokens goes from 57.4 to 58.2 us a call.)
 //
 // Bound: HBM for prompts. 8192 tokens of 32 + 8 heads of 128, bf16, norms: rotation 36.7 us for 168 MB
-// (4.6 TB/s, a large copy's 4.88), append 45.4 us for 201 MB. One token: 3.0 and 4.7 us, a launch.
+// (4.6 TB/s, a large copy's 4.88), append 44.5 us for 201 MB. One token: 3.0 and 4.6 us, a launch.
 // A decode batch's values are single 2-byte stores a column (2048 sequences: 46 us, five times its bytes'
 // time); that is what the transposed layout costs, and the attention reads each of them hundreds of times.
 #include <math.h>

@@ -23,7 +23,9 @@
 // gathered from the row (256 MB of cache hold it) and the cut found among them by steps of their keys; the
 // chunks' kept masses give the chunk of the draw, and its tokens the draw. Rows that none of this fits (lists
 // and bins that overflow, a cut below 32 temperatures, infinite logits) take the long way, row_cut: the cut
-// digit by digit (11, 11, 10 bits of the logit's ordered bits), each by a pass over the row.
+// digit by digit (11, 11, 10 bits of the logit's ordered bits), each by a pass over the row. Flat rows are among them: a
+// bin's tokens overflow from a temperature of about 1.5 on at 128256 tokens of normal logits (deviation 2.5), and from 1.2
+// on at 262144 (top-p of one row 62 us by bins, 324 the long way, 624 at 262144; 192 rows 109 and 403).
 //
 // Bound: the chunk kernel by HBM and its fp64 weights together (192 rows of 128256 tokens, 98 MB: greedy 16 us,
 // the rate of a read; top_k 29; sums alone 34; bins too 40-44), the finishing kernel by the chain of barriers
@@ -426,7 +428,7 @@ __device__ __forceinline__ void row_cut(const Args& a, const Ask& q, const Weigh
     sh.count[i] = 0;
   }
   __syncthreads();
-  // four tiles a thread: ties first, then the tiles' masses with the ties that stay
+  // eight tiles a thread: ties first, then the tiles' masses with the ties that stay
   constexpr int kPer = kTiles / kThreads;
   int tie[kPer], tsum = 0;
 #pragma unroll
