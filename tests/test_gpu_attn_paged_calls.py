@@ -117,3 +117,43 @@ def test_caps_at_the_ends_of_fp32(sr, cap):
         more = 2.0 ** -8 * (np.abs(want) + serve.attn_paged(oracle.widen_bf16(q), kp, vp & 0x7fff, table, before, start,
                                                             softcap=float(np.float32(cap)))) if new == [80] else 0.0
         assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + more + 0.002 * rms).all(), (cap, new)
+
+
+@pytest.mark.parametrize("before,new,page,kw", [
+    ([100], [300], 24, dict()), ([100], [300], 24, dict(window=130, softcap=20.0)), ([3000, 90], [1, 3], 8, dict()),
+    ([700], [20], 64, dict(window=600)), ([0], [40], 16, dict())])
+@pytest.mark.parametrize("qt", ["f32", "bf16"])
+def test_infinities_and_nans_that_are_seen(sr, before, new, page, kw, qt):
+    """An infinite value stays in its column, a key of NaN in the rows and heads that see it; everything else is as without
+    them, whichever rows the matrix units' pieces spoil."""
+    h, hkv, hd = 8, 2, 96
+    rng, q, kp, vp, table, start = _inputs(31, before, new, page, h, hkv, hd)
+    seen = before[0] + new[0]
+    at = lambda row: (table[0, row // page], row % page)
+    v_row, k_row = (seen * 2 // 3, seen - new[0] // 2 - 1) if kw.get("window", 999) > 200 else (seen - 260, seen - 60)
+    qq = oracle.widen_bf16(q).astype(np.float32)
+    want = serve.attn_paged(qq, kp, vp, table, before, start, **kw)
+    more = 2.0 ** -8 * (np.abs(want) + serve.attn_paged(qq, kp, vp & 0x7fff, table, before, start, **kw)) if qt == "bf16" else 0.0
+    pg, off = at(v_row)
+    v2 = vp.copy()
+    v2[pg, 0, 5, off], v2[pg, 0, 70, off] = bf16_bits(np.array([np.inf, -np.inf], np.float32))
+    k2 = kp.copy()
+    pg, off = at(k_row)
+    k2[pg, 1, off, 17] = bf16_bits(np.array([np.nan], np.float32))[0]
+    out = sr.sirius_attn_paged(dev_f32(qq) if qt == "f32" else dev_bf16(q), dev_bf16(k2), dev_bf16(v2), dev_i32(table),
+                               dev_i32(np.array(before)), tok_start=dev_i32(start), **kw)
+    got = (host(out) if qt == "f32" else oracle.widen_bf16(host(out))).astype(np.float64)
+    row = np.concatenate([p + np.arange(n) for p, n in zip(before, new)])
+    mine = np.arange(sum(new)) < new[0]
+    window = kw.get("window") or 1 << 30
+    sees = lambda r: mine & (row >= r) & (row < r + window)
+    heads = np.arange(h) // (h // hkv)
+    bad = np.zeros(got.shape, bool)
+    bad[np.ix_(sees(v_row), heads == 0, [5, 70])] = True
+    bad[np.ix_(sees(k_row), heads == 1)] = True
+    assert (got[np.ix_(sees(v_row), heads == 0, [5])] == np.inf).all() and (got[np.ix_(sees(v_row), heads == 0, [70])] == -np.inf).all()
+    assert np.isnan(got[np.ix_(sees(k_row), heads == 1)]).all()
+    rms = float(np.sqrt(np.mean(want ** 2)))
+    tol = (2.0 ** -8 * np.abs(want) + more + 0.002 * rms) if qt == "bf16" else 1e-4 * rms
+    ok = np.abs(got - want) <= tol
+    assert ok[~bad].all(), float(np.max(np.abs(got - want)[~bad])) / rms
